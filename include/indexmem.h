@@ -439,6 +439,123 @@ int im_set_scores(im_ctx* ctx, int layer, int n_seq, const float* scores, int64_
 int im_state_export_head(im_ctx* ctx, int layer, int seq, int head, int which, void* host_buf, size_t bytes);
 int im_state_import_head(im_ctx* ctx, int layer, int seq, int head, int which, const void* host_buf, size_t bytes);
 
+/*
+ * A paged KV cache held in 4 bits, and its operators (no counterpart in the paper: a smaller cache for the entries that an
+ * eviction keeps).  Usable without a context; the state is the caller's device memory, described by two small structs.
+ *
+ * Format.  A cached token holds, for each KV head, head_dim key and head_dim value channels in blocks of 16: a 4-bit code
+ * e2m1 per channel (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign) and an 8-bit scale e4m3 per block.  value = code * scale *
+ * 2^exp with one exponent per KV head.  Storing x: scale = e4m3(max |x 2^-exp| / 6), code = e2m1(x 2^-exp / scale), both
+ * to the nearest (ties to even) and saturating; a block whose scale rounds to 0 holds zeros; a NaN is held as 0 and an
+ * infinity as the largest value, and both set IM_KV4_NONFINITE.  What a cache holds is always finite.
+ *   pool  [n_pages][n_kv_heads][page_size / 16] groups of 16 tokens of 18 * head_dim bytes each: [16][head_dim / 2] key
+ *         codes (the even channel in the low half of a byte), [16][head_dim / 16] key scales, then the values likewise.
+ * Maps.  Which pages hold which sequence is said by a map: refs int32 [n_pages] (how many sequences hold a page; 0 = free),
+ * table int32 [n_seqs][max_pages] (the pages of a sequence in order) and lens int32 [n_seqs] (its tokens).  An empty cache
+ * has refs and lens zero.  Several maps may share a pool and its refs (the layers of a model, say: each a block of rows of
+ * one large table).  Calls that change a map read it from `from` and write it to `to`: the same arrays (the state advances
+ * in place), or other arrays that do not overlap them (`from` stays as it is, and so does what its sequences hold; a part-full
+ * last page receives the new tokens behind them).  Pages that such a call needs are the
+ * lowest free ones (by `from`), handed out in order of sequence; a page that the call releases is not handed out by the
+ * same call.  Where a row of `to` has no page, its entry is left as it was.
+ * A call that cannot be made (too few free pages, a sequence that would outgrow max_pages, cu or the map inconsistent)
+ * changes nothing: `to` becomes a copy of `from`, no byte of the pool is written, and the reason is set in *status.
+ * All device pointers belong to the current device, all work is enqueued on `cuda_stream`; nothing synchronises, allocates
+ * or depends on the host having seen a map, so every call can be captured into a CUDA graph and replayed.  A workspace
+ * (256-byte aligned) holds what one call passes between its kernels: calls that may run at the same time, captured
+ * ones included, need one each.  The sizes must fit: n_seqs <= 65535, n_kv_heads <= 256, n_pages * page_size and max_pages
+ * * page_size below 2^31, max_pages * page_size * n_kv_heads * n_seqs below 2^36.
+ */
+typedef enum im_dtype { IM_BF16 = 0, IM_F16 = 1, IM_F32 = 2 } im_dtype;
+
+/* bits of *status (sticky: the library only sets them) */
+typedef enum im_kv4_status {
+  IM_KV4_NO_PAGES = 1,  /* the call needed more pages than are free, or a longer row than max_pages: nothing changed */
+  IM_KV4_BAD_MAP = 2,   /* a length, page id, cu or parent out of range: nothing changed, or that page / row was skipped */
+  IM_KV4_NONFINITE = 4, /* a key or value handed to im_kv4_append was not finite                                         */
+  IM_KV4_TIMEOUT = 8    /* a bounded device-side wait gave up: the outputs of that call are undefined                    */
+} im_kv4_status;
+
+typedef struct im_kv4 {
+  void* pool;            /* dev, 16-byte aligned, n_pages * im_kv4_page_bytes(...) bytes                       */
+  const int32_t* k_exp;  /* dev int32 [n_kv_heads] in [-60, 60], or NULL: all 0                                */
+  const int32_t* v_exp;
+  int32_t* status;       /* dev int32 [1], bits of im_kv4_status                                               */
+  int32_t n_pages, page_size; /* page_size 16, 32, 64 or 128 tokens                                            */
+  int32_t n_kv_heads, head_dim; /* head_dim 64, 128 or 256                                                     */
+  int32_t n_seqs, max_pages;  /* rows of a map and their length                                                */
+} im_kv4;
+
+typedef struct im_kv4_map {
+  int32_t* refs;
+  int32_t* table;
+  int32_t* lens;
+} im_kv4_map;
+
+/* Bytes of one page; 0 if the sizes are not supported. */
+size_t im_kv4_page_bytes(int n_kv_heads, int head_dim, int page_size);
+
+/* Bytes of workspace for a call: op 0 im_kv4_append (n = n_tokens), 1 im_kv4_attention (n = n_tokens), 2 im_kv4_compact
+ * (n = keep_stride; n_q_heads is read by op 1 alone).  0 if the arguments are invalid. */
+size_t im_kv4_workspace_bytes(const im_kv4* cache, int op, int n, int n_q_heads);
+
+/*
+ * Appends tokens cu_new[i] .. cu_new[i + 1] - 1 of k and v to sequence i, quantised.
+ *   k, v    dev [n_tokens][n_kv_heads][head_dim], dtype IM_BF16 or IM_F16; k_stride / v_stride elements from one token to
+ *           the next (0: dense), multiples of 8, base 16-byte aligned
+ *   cu_new  dev int32 [n_seqs + 1], ascending, within [0, n_tokens]; NULL: one token for each sequence (n_tokens = n_seqs).
+ *           Tokens before cu_new[0] and from cu_new[n_seqs] on belong to nobody and are ignored.
+ * A sequence that gets tokens while its last page is part full and held by others too takes a page of its own first and
+ * copies that page's tokens: a fork (im_kv4_fork) shares pages until it writes.
+ */
+int im_kv4_append(const im_kv4* cache, const im_kv4_map* from, const im_kv4_map* to, int dtype, const void* k,
+                  long long k_stride, const void* v, long long v_stride, int n_tokens, const int32_t* cu_new,
+                  void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Softmax attention over the cache: query tokens cu_q[i] .. cu_q[i + 1] - 1 attend to sequence i (out_j = sum_t softmax_t(scale
+ * * q_j . k_t) v_t, query head j on KV head j / (n_q_heads / n_kv_heads)).
+ *   q       dev [n_tokens][n_q_heads][head_dim], dtype IM_BF16 or IM_F16, q_stride as k_stride above
+ *   cu_q    dev int32 [n_seqs + 1] as cu_new above; NULL: one query token for each sequence (n_tokens = n_seqs)
+ *   max_q   the largest number of query tokens of a sequence (host; it chooses the kernels: a wrong one costs time only)
+ *   causal  1: the queries of a sequence are its last tokens, the j-th of n sees the first len - n + j + 1 entries; 0: all
+ *   out     dev [n_tokens][n_q_heads][head_dim] in q's type, or float32 (out_f32 = 1), dense
+ *   lse     dev float32 [n_tokens][n_q_heads], log of the sum of exponentials, or NULL
+ * A query that sees nothing (an empty sequence, more queries than entries) gets zeros and lse = -inf.  Rows of out and lse that belong
+ * to no sequence are left as they were.  softmax_scale 0 => 1/sqrt(head_dim), otherwise positive.
+ */
+int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int dtype, const void* q, long long q_stride,
+                     int n_tokens, const int32_t* cu_q, int max_q, int n_q_heads, float softmax_scale, int causal, void* out,
+                     int out_f32, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Reads entries back: row r of cu_rows[i] .. cu_rows[i + 1] - 1 receives entry slots[r] of sequence i (keys and values of
+ * an evicted set, for instance: what im_topb_select's keep leaves out).
+ *   slots    dev int32 [n_rows]; NULL: row cu_rows[i] + j reads entry j.  An entry outside [0, len) reads as zeros.
+ *   cu_rows  dev int32 [n_seqs + 1] as cu_new above; NULL: one row for each sequence (n_rows = n_seqs)
+ *   k, v     dev [n_rows][n_kv_heads][head_dim] in `dtype` (IM_BF16, IM_F16, IM_F32), dense; either may be NULL
+ */
+int im_kv4_gather(const im_kv4* cache, const im_kv4_map* map, int n_rows, const int32_t* cu_rows, const int32_t* slots,
+                  int dtype, void* k, void* v, void* cuda_stream);
+
+/*
+ * Forks, reorders and frees sequences: row i of `to` becomes row parent[i] of `from` (parent[i] = i: stays; -1: empty).
+ * No byte of the pool moves; pages are shared, and freed when nobody holds them.
+ *   parent  dev int32 [n_seqs], -1 .. n_seqs - 1; any other value sets IM_KV4_BAD_MAP and counts as i
+ * The rows may change places, so to->table and to->lens must not overlap those of `from`; to->refs may be from->refs.
+ */
+int im_kv4_fork(const im_kv4* cache, const im_kv4_map* from, const im_kv4_map* to, const int32_t* parent,
+                void* cuda_stream);
+
+/*
+ * Keeps the entries t of sequence i with keep[i][t] != 0, in order, and drops the others (an eviction: keep as
+ * im_topb_select writes it).  Pages ahead of a sequence's first dropped entry stay as they are, shared ones among them;
+ * the survivors behind it move to free pages and the pages they came from are released.  A sequence that drops nothing is left alone.
+ *   keep  dev uint8 [n_seqs][keep_stride]; keep_stride is at least the longest sequence (a longer one: IM_KV4_BAD_MAP)
+ */
+int im_kv4_compact(const im_kv4* cache, const im_kv4_map* from, const im_kv4_map* to, const uint8_t* keep,
+                   int keep_stride, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Thread-local description of the last error returned on this thread ("" if none). */
 const char* im_last_error(void);
 

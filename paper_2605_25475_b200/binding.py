@@ -75,11 +75,33 @@ _lib.im_event_count.argtypes = [_vp, _i32, C.POINTER(C.c_int64)]
 _lib.im_attention_noalloc.argtypes = [_vp, _vp, _vp, _i32, _i32, _i32, _i32, C.c_float, _vp, _vp]
 _lib.im_last_error.restype = C.c_char_p
 
+
+class im_kv4(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("status", C.c_void_p)] + \
+        [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "n_seqs", "max_pages")]
+
+
+class im_kv4_map(C.Structure):
+    _fields_ = [("refs", C.c_void_p), ("table", C.c_void_p), ("lens", C.c_void_p)]
+
+
+_i64 = C.c_longlong
+_lib.im_kv4_page_bytes.argtypes = [_i32, _i32, _i32]
+_lib.im_kv4_page_bytes.restype = _sz
+_lib.im_kv4_workspace_bytes.argtypes = [_vp, _i32, _i32, _i32]
+_lib.im_kv4_workspace_bytes.restype = _sz
+_lib.im_kv4_append.argtypes = [_vp, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _sz, _vp]
+_lib.im_kv4_attention.argtypes = [_vp, _vp, _i32, _vp, _i64, _i32, _vp, _i32, _i32, C.c_float, _i32, _vp, _i32, _vp, _vp, _sz, _vp]
+_lib.im_kv4_gather.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp]
+_lib.im_kv4_fork.argtypes = [_vp, _vp, _vp, _vp, _vp]
+_lib.im_kv4_compact.argtypes = [_vp, _vp, _vp, _vp, _i32, _vp, _sz, _vp]
+
 EXPORTED = ("im_workspace_bytes", "im_create", "im_destroy", "im_reset", "im_prefill_chunk", "im_decode_step",
             "im_set_weights", "im_get_weights", "im_state_export", "im_state_import", "im_topb_select",
             "im_status", "im_launch_count", "im_get_config", "im_last_error", "im_profile_begin", "im_profile_end", "im_set_option", "im_attention_noalloc", "im_event_count", "im_prefill_chunk_attend",
             "im_set_scores", "im_state_export_head", "im_state_import_head", "im_decode_stack",
-            "im_decode_stack_events")
+            "im_decode_stack_events", "im_kv4_page_bytes", "im_kv4_workspace_bytes", "im_kv4_append", "im_kv4_attention",
+            "im_kv4_gather", "im_kv4_fork", "im_kv4_compact")
 
 
 def _check(rc: int):
@@ -551,3 +573,208 @@ class IndexMem:
             im_state_import(self.ctx, layer, seq, IM_S_KIDX, _bf16_bits(torch.from_numpy(np.asarray(kidx, np.float32))))
             im_state_import(self.ctx, layer, seq, IM_S_K, _bf16_bits(torch.from_numpy(np.asarray(K, np.float32))))
             im_state_import(self.ctx, layer, seq, IM_S_V, _bf16_bits(torch.from_numpy(np.asarray(V, np.float32))))
+
+
+# ------------------------------------------------------------------ paged KV cache held in 4 bits
+IM_BF16, IM_F16, IM_F32 = 0, 1, 2
+IM_KV4_NO_PAGES, IM_KV4_BAD_MAP, IM_KV4_NONFINITE, IM_KV4_TIMEOUT = 1, 2, 4, 8
+_DTYPE_IDS = {torch.bfloat16: IM_BF16, torch.float16: IM_F16, torch.float32: IM_F32}
+
+
+def im_kv4_page_bytes(n_kv_heads: int, head_dim: int, page_size: int) -> int:
+    return int(_lib.im_kv4_page_bytes(n_kv_heads, head_dim, page_size))
+
+
+class KV4Map:
+    """Which pages hold which sequence: refs int32 [n_pages], table int32 [n_seqs, max_pages], lens int32 [n_seqs]."""
+
+    def __init__(self, refs: torch.Tensor, table: torch.Tensor, lens: torch.Tensor):
+        for t, dim in ((refs, 1), (table, 2), (lens, 1)):
+            if not (t.is_cuda and t.dtype == torch.int32 and t.dim() == dim and t.is_contiguous() and t.device == refs.device):
+                raise ValueError("a map is three contiguous int32 CUDA tensors on one device: refs [n_pages], table [n_seqs, "
+                                 "max_pages], lens [n_seqs]")
+        if table.shape[0] != lens.shape[0]:
+            raise ValueError("table and lens of a map have one row per sequence")
+        self.refs, self.table, self.lens = refs, table, lens
+        self._c = im_kv4_map(refs.data_ptr(), table.data_ptr(), lens.data_ptr())
+        self._p = C.addressof(self._c)
+
+    def clone(self) -> "KV4Map":
+        return KV4Map(self.refs.clone(), self.table.clone(), self.lens.clone())
+
+
+class KV4Cache:
+    """A paged KV cache held in 4 bits (``im_kv4`` in the header): e2m1 codes in blocks of 16 channels with an e4m3 scale
+    each.  Owns the pool and its map unless they are handed in; methods map one-to-one onto the ``im_kv4_*`` calls.
+
+    Calls go to the current stream of the cache's device and never synchronise.  A call that changes the map does so in
+    place, or reads it from ``map`` and writes ``to`` (other tensors) where that is given.  ``status()`` says what the
+    device found (bits ``IM_KV4_*``); a call that could not be made has left everything as it was."""
+
+    def __init__(self, n_seqs, max_pages, n_pages, n_kv_heads, head_dim, page_size=64, *, k_exp=None, v_exp=None,
+                 device="cuda:0", pool=None, map=None, status=None):
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("a KV4Cache lives on a CUDA device (there is no CPU fallback)")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.n_seqs, self.max_pages, self.n_pages = n_seqs, max_pages, n_pages
+        self.n_kv_heads, self.head_dim, self.page_size = n_kv_heads, head_dim, page_size
+        page = im_kv4_page_bytes(n_kv_heads, head_dim, page_size)
+        if page == 0 or min(n_seqs, max_pages, n_pages) < 1:
+            raise IndexMemError(IM_ERR_ARG, "unsupported sizes of a 4-bit cache")
+        i32 = {"dtype": torch.int32, "device": self.device}
+        self.pool = torch.empty(n_pages * page, dtype=torch.uint8, device=self.device) if pool is None else pool
+        _dev(self.pool, torch.uint8, n_pages * page, "pool")
+        self.map = KV4Map(torch.zeros(n_pages, **i32), torch.full((n_seqs, max_pages), -1, **i32), torch.zeros(n_seqs, **i32)) \
+            if map is None else map
+        self._status = torch.zeros(1, **i32) if status is None else status
+        self.k_exp, self.v_exp = k_exp, v_exp
+        for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+            if t is not None:
+                _dev(t, torch.int32, n_kv_heads, name)
+        self._check_map(self.map)
+        _dev(self._status, torch.int32, 1, "status")
+        for t in (self.pool, self._status, self.k_exp, self.v_exp):
+            if t is not None and t.device != self.device:
+                raise ValueError("the tensors of a KV4Cache are on its device")
+        self._c = im_kv4(self.pool.data_ptr(), _ptr(k_exp), _ptr(v_exp), self._status.data_ptr(), n_pages, page_size, n_kv_heads,
+                         head_dim, n_seqs, max_pages)
+        self._p = C.addressof(self._c)
+        self._ws_bytes = {}
+
+    def rows(self, first: int, last: int) -> "KV4Cache":
+        """Sequences first .. last - 1 as a cache of their own over the same pool (one layer's rows of a model's cache)."""
+        if not 0 <= first < last <= self.n_seqs:
+            raise ValueError("rows out of range")
+        m = self.map
+        return KV4Cache(last - first, self.max_pages, self.n_pages, self.n_kv_heads, self.head_dim, self.page_size, k_exp=self.k_exp,
+                        v_exp=self.v_exp, device=self.device, pool=self.pool, map=KV4Map(m.refs, m.table[first:last], m.lens[first:last]),
+                        status=self._status)
+
+    # ---- helpers
+    def _check_map(self, m: KV4Map):
+        if m.refs.device != self.device or m.refs.shape[0] != self.n_pages or tuple(m.table.shape) != (self.n_seqs, self.max_pages):
+            raise ValueError(f"the map does not belong to this cache ({self.n_pages} pages, {self.n_seqs} sequences of up to "
+                             f"{self.max_pages} pages, {self.device})")
+        return m
+
+    def _call(self, fn, *args):
+        d = self.device.index
+        if torch.cuda.current_device() == d:
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        else:
+            with torch.cuda.device(d):
+                rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        if rc != IM_OK:
+            _check(rc)
+
+    def _workspace(self, op, n, heads=0):
+        """(tensor, bytes): from torch's allocator for every call, so that calls that overlap have one each."""
+        nbytes = self._ws_bytes.get((op, n, heads))
+        if nbytes is None:
+            nbytes = int(_lib.im_kv4_workspace_bytes(self._p, op, n, heads))
+            if nbytes == 0:
+                _check(IM_ERR_ARG)
+            if len(self._ws_bytes) >= 256:
+                self._ws_bytes.clear()
+            self._ws_bytes[op, n, heads] = nbytes
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device), nbytes
+
+    def _rows_of(self, t, heads, name):
+        """A [n, heads, head_dim] tensor whose tokens may be strided (a slice of a fused projection): its token stride."""
+        if t.device != self.device or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.stride(2) != 1 or \
+                (heads > 1 and t.stride(1) != self.head_dim) or (t.shape[0] > 1 and t.stride(0) < heads * self.head_dim):
+            raise ValueError(f"{name}: need [tokens, {heads}, {self.head_dim}] on {self.device}, dense within a token, got "
+                             f"{tuple(t.shape)} {t.stride()} {t.device}")
+        return t.stride(0) if t.shape[0] > 1 else 0
+
+    def _starts(self, cu, n, what):
+        """cu (int32 [n_seqs + 1] on the device) or None: one of each sequence."""
+        if cu is None:
+            if n != self.n_seqs:
+                raise ValueError(f"{what}: without cu there is one for each of the {self.n_seqs} sequences, got {n}")
+            return 0
+        if cu.device != self.device or cu.dtype != torch.int32 or cu.numel() != self.n_seqs + 1 or not cu.is_contiguous():
+            raise ValueError(f"{what}: cu must be a contiguous int32 tensor of {self.n_seqs + 1} starts on {self.device}")
+        return cu.data_ptr()
+
+    def _maps(self, map, to):
+        a = self.map if map is None else self._check_map(map)
+        return a, a if to is None else self._check_map(to)
+
+    # ---- calls
+    def append(self, k, v, cu_new=None, *, map=None, to=None):
+        """k, v bf16 / f16 [n_tokens, n_kv_heads, head_dim]: tokens cu_new[i] .. cu_new[i + 1] - 1 go to sequence i."""
+        n = k.shape[0]
+        ks, vs = self._rows_of(k, self.n_kv_heads, "k"), self._rows_of(v, self.n_kv_heads, "v")
+        if v.shape[0] != n or v.dtype != k.dtype or k.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("k and v: as many tokens of one type, bf16 or f16")
+        a, b = self._maps(map, to)
+        ws, nbytes = self._workspace(0, n)
+        self._call(_lib.im_kv4_append, self._p, a._p, b._p, _DTYPE_IDS[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, n,
+                   self._starts(cu_new, n, "append"), ws.data_ptr(), nbytes)
+
+    def attend(self, q, cu_q=None, max_q=1, *, softmax_scale=0.0, causal=True, out=None, out_f32=False, return_lse=False, map=None):
+        """Attention of q bf16 / f16 [n_tokens, n_q_heads, head_dim] over the cache: tokens cu_q[i] .. cu_q[i + 1] - 1 see
+        sequence i, whose last tokens they are if causal.  max_q: the largest number of them (it chooses the kernels).
+        Returns out (q's type, or float32), with return_lse also the log of the softmax's sum, float32 [n_tokens, n_q_heads]."""
+        n, H = q.shape[0], q.shape[1]
+        qs = self._rows_of(q, H, "q")
+        if q.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("q: bf16 or f16")
+        dtype = torch.float32 if out_f32 else q.dtype
+        if out is None:
+            out = torch.empty((n, H, self.head_dim), dtype=dtype, device=self.device)
+        elif out.device != self.device or out.dtype != dtype or tuple(out.shape) != (n, H, self.head_dim) or not out.is_contiguous():
+            raise ValueError(f"out: need a contiguous {dtype} tensor {(n, H, self.head_dim)} on {self.device}")
+        lse = torch.empty((n, H), dtype=torch.float32, device=self.device) if return_lse else None
+        m = self.map if map is None else self._check_map(map)
+        ws, nbytes = self._workspace(1, n, H)
+        self._call(_lib.im_kv4_attention, self._p, m._p, _DTYPE_IDS[q.dtype], q.data_ptr(), qs, n, self._starts(cu_q, n, "attend"),
+                   max_q, H, softmax_scale, 1 if causal else 0, out.data_ptr(), 1 if out_f32 else 0, _ptr(lse), ws.data_ptr(), nbytes)
+        return (out, lse) if return_lse else out
+
+    def gather(self, slots=None, cu_rows=None, *, n_rows=None, dtype=torch.bfloat16, map=None):
+        """(k, v) [n_rows, n_kv_heads, head_dim]: entry slots[r] of the sequence that row r belongs to by cu_rows; without
+        slots (then n_rows is given) row cu_rows[i] + j reads entry j.  An entry that is not there reads as zeros."""
+        if slots is not None:
+            if slots.device != self.device or slots.dtype != torch.int32 or slots.dim() != 1 or not slots.is_contiguous():
+                raise ValueError(f"slots: need a contiguous int32 vector on {self.device}")
+            if n_rows not in (None, slots.shape[0]):
+                raise ValueError("n_rows and slots disagree")
+            n_rows = slots.shape[0]
+        if n_rows is None or n_rows < 0 or dtype not in _DTYPE_IDS:
+            raise ValueError("gather: needs slots or n_rows, and a type of bf16, f16 or float32")
+        k = torch.empty((n_rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
+        m = self.map if map is None else self._check_map(map)
+        self._call(_lib.im_kv4_gather, self._p, m._p, n_rows, self._starts(cu_rows, n_rows, "gather"), _ptr(slots), _DTYPE_IDS[dtype],
+                   k.data_ptr(), v.data_ptr())
+        return k, v
+
+    def fork(self, parent, *, map=None, to=None):
+        """Row i becomes what row parent[i] was (int32 [n_seqs]; i: stays, -1: emptied).  In place it goes through a copy of
+        the table."""
+        if parent.device != self.device or parent.dtype != torch.int32 or parent.numel() != self.n_seqs or not parent.is_contiguous():
+            raise ValueError(f"parent: need a contiguous int32 tensor of {self.n_seqs} rows on {self.device}")
+        a, b = self._maps(map, to)
+        if b is a:
+            a = KV4Map(b.refs, b.table.clone(), b.lens.clone())
+        self._call(_lib.im_kv4_fork, self._p, a._p, b._p, parent.data_ptr())
+
+    def compact(self, keep, *, map=None, to=None):
+        """Keeps the entries t of sequence i with keep[i, t] != 0 (uint8 [n_seqs, n], as im_topb_select returns it)."""
+        if keep.device != self.device or keep.dtype != torch.uint8 or keep.dim() != 2 or keep.shape[0] != self.n_seqs or \
+                keep.shape[1] < 1 or not keep.is_contiguous():
+            raise ValueError(f"keep: need a contiguous uint8 tensor [{self.n_seqs}, n] on {self.device}")
+        a, b = self._maps(map, to)
+        ws, nbytes = self._workspace(2, keep.shape[1])
+        self._call(_lib.im_kv4_compact, self._p, a._p, b._p, keep.data_ptr(), keep.shape[1], ws.data_ptr(), nbytes)
+
+    def status(self, clear=False) -> int:
+        """What the device found so far (bits IM_KV4_*); synchronises."""
+        st = int(self._status.item())
+        if clear:
+            self._status.zero_()
+        return st
