@@ -17,7 +17,7 @@ struct Kv4 {
   int n_pages, ps, Hkv, d, n_seqs, max_pages;
 };
 
-__host__ __device__ __forceinline__ int kv4_group_bytes(int d) { return 18 * d; }  // 16 tokens, keys and values
+constexpr int kv4_group_bytes(int d) { return 18 * d; }  // 16 tokens, keys and values
 __device__ __forceinline__ size_t kv4_group_index(const Kv4& c, int page, int h, int group) {
   return ((size_t)page * c.Hkv + h) * (c.ps >> 4) + group;
 }

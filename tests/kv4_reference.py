@@ -121,9 +121,10 @@ class Cache:
         return True
 
     def attend(self, q, cu, scale, causal):
-        """(out, lse, weight, spread): weight = sum_t p_t |v_t| per output, spread = max_t scale sum_c |q_c k_tc| per row."""
+        """(out, lse, weight, spread, every): per output weight = sum_t p_t |v_t| and every = sum_t |v_t|, per row spread =
+        max_t scale sum_c |q_c k_tc|."""
         T, H, d = q.shape
-        out, lse = np.zeros((T, H, d)), np.full((T, H), -np.inf)
+        out, lse, every = np.zeros((T, H, d)), np.full((T, H), -np.inf), np.zeros((T, H, d))
         weight, spread = np.zeros((T, H, d)), np.zeros((T, H))
         for i in range(self.n):
             K, V = self.kv(i)
@@ -141,5 +142,6 @@ class Cache:
                     lse[cu[i] + j, h] = m + np.log(p.sum())
                     p /= p.sum()
                     out[cu[i] + j, h], weight[cu[i] + j, h] = p @ V[:sees, g], p @ np.abs(V[:sees, g])
+                    every[cu[i] + j, h] = np.abs(V[:sees, g]).sum(0)
                     spread[cu[i] + j, h] = (np.abs(K[:sees, g]) @ np.abs(x)).max() * scale
-        return out, lse, weight, spread
+        return out, lse, weight, spread, every

@@ -83,12 +83,13 @@ def check_attention(r, q, cu, sc, causal, o, lse):
     the sums.  Scores: products are exact, a sum of d of them in float32 errs by at most (d + 4) 2^-23 of the sum of their
     absolute values (`spread`; any order, truncating adders); the base-2 exponent's argument, formed with a multiply-add from a
     rounded scale, by 4 x 2^-24 of its size, which `spread` bounds too, and exp2 by 2^-22.  p has one error e and the sum that
-    divides it has the same: 2 e.  p is kept in f16 for bf16 outputs (2^-11, the running maximum up to 2^8 above or below it
-    included: f16 is a floating type) and in two f16 terms otherwise (2^-20).  Sums over L entries in float32, scaled at most
-    once a tile: (L / 16 + 64) 2^-22 of the sum of absolute values covers any split."""
+    divides it has the same: 2 e.  p is kept in f16 for bf16 outputs (2^-11) and in two f16 terms otherwise (2^-20); a p
+    below f16's normal range is off by half of f16's smallest step, 2^-25, while the row's largest p is kept as 2^7 and
+    the sum that divides is no less: 2^-32 sum_t |v_t|.  Sums over L entries in float32, scaled at most once a tile: (L / 16 + 64)
+    2^-22 of the sum of absolute values covers any split."""
     d = q.shape[2]
     qn = q.double().cpu().numpy()
-    out, ls, weight, spread = r.attend(qn, cu, sc, causal)
+    out, ls, weight, spread, every = r.attend(qn, cu, sc, causal)
     L = max(1, int(r.lens.max()))
     e = ((d + 4) * 2.0 ** -23 + 2.0 ** -22) * spread[..., None] + 2.0 ** -22
     sums = (L / 16 + 64) * 2.0 ** -22
@@ -96,7 +97,7 @@ def check_attention(r, q, cu, sc, causal, o, lse):
     half = torch.finfo(o.dtype).eps / 2
     tiny = torch.finfo(o.dtype).tiny * torch.finfo(o.dtype).eps  # below the normal range steps are of this size
     got = o.double().cpu().numpy()
-    bound = half * np.abs(out) + (1 + half) * A * weight + tiny
+    bound = half * np.abs(out) + (1 + half) * (A * weight + 2.0 ** -32 * every) + tiny
     bad = ~(np.abs(got - out) <= bound)
     assert not bad.any(), f"{bad.sum()} outputs off, worst {np.nanmax(np.abs(got - out) / bound)} of the bound"
     gl = lse.double().cpu().numpy()
