@@ -15,7 +15,8 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int PLAN_CTAS = 8, PLAN_THREADS = 512, PLAN_WARPS = PLAN_THREADS / 32;
-constexpr int SCAN_THREADS = 512;
+constexpr int SCAN_THREADS = 1024;
+constexpr int PLAN_ONE_CTA_PAGES = 8192;
 enum { PLAN_APPEND = 0, PLAN_COMPACT = 1 };
 
 // What a plan hands to the kernels behind it (in the caller's workspace; every word that is read is written by the same call).
@@ -69,13 +70,13 @@ __device__ __forceinline__ int new_tokens(const int32_t* cu, int i, int n_tokens
 // are counted and listed by shares.  Phases are separated by cluster barriers, so that with from == to nothing is written
 // before everybody has read what the decision depends on.
 template <int MODE>
-__global__ void __cluster_dims__(PLAN_CTAS, 1, 1) __launch_bounds__(PLAN_THREADS)
+__global__ void __launch_bounds__(PLAN_THREADS)
 k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu, int n_tokens, PlanWs ws) {
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ long long s_warp[PLAN_WARPS];
   __shared__ int s_free[PLAN_WARPS];
   __shared__ int s_count;
-  const int rank = (int)cluster.block_rank(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_release();
   if (MODE == PLAN_COMPACT) pdl_wait();  // (the scan kernel's counts)
   // ---- what each sequence needs
@@ -121,7 +122,7 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
   bad = __syncthreads_or(bad);
   full = __syncthreads_or(full);
   // ---- free pages of this CTA's share, in runs per warp
-  const int share = (c.n_pages + PLAN_CTAS - 1) / PLAN_CTAS;
+  const int share = (c.n_pages + ctas - 1) / ctas;
   const int p0 = min(c.n_pages, rank * share), p1 = min(c.n_pages, p0 + share);
   const int run = ((p1 - p0 + PLAN_WARPS - 1) / PLAN_WARPS + 31) & ~31;
   const int w0 = min(p1, p0 + warp * run), w1 = min(p1, w0 + run);
@@ -147,7 +148,7 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
   cluster.sync();
   int first = 0, free_pages = 0;
   if (want)
-    for (int r = 0; r < PLAN_CTAS; ++r) {
+    for (int r = 0; r < ctas; ++r) {
       const int n = *cluster.map_shared_rank(&s_count, r);
       if (r < rank) first += n;
       free_pages += n;
@@ -175,7 +176,7 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
   }
   cluster.sync();  // (also the last read of another CTA's shared memory)
   // ---- rows
-  for (int i = rank * PLAN_WARPS + warp; i < c.n_seqs; i += PLAN_CTAS * PLAN_WARPS) {
+  for (int i = rank * PLAN_WARPS + warp; i < c.n_seqs; i += ctas * PLAN_WARPS) {
     const int L = from.lens[i];
     const size_t row = (size_t)i * c.max_pages;
     const int held = L < 0 ? 0 : (int)min((long long)c.max_pages, ((long long)L + c.ps - 1) / c.ps);
@@ -248,51 +249,50 @@ __device__ __forceinline__ float2 two_floats<__half>(uint32_t v) {
   return kv4_unpack_f16(v);
 }
 
-// One thread per block of 16 channels: thread index = ((2 h + which) * n_tokens + t) * (d / 16) + block, so that a warp
-// reads whole rows and writes the code rows of neighbouring tokens of one head, which lie side by side.  The last
-// n_seqs blocks of the grid copy the tokens of shared last pages.  The loads and the quantiser run ahead of the wait for
-// the plan.
+// One thread per block of 16 channels; grid.y = (head, keys / values), grid.x over (token, block): a warp reads whole rows
+// and writes the code rows of neighbouring tokens of one head, which lie side by side.  The rows of the grid behind those
+// copy the tokens of shared last pages.  The loads and the quantiser run ahead of the wait for the plan.
 constexpr int STORE_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(STORE_THREADS)
 k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, const T* __restrict__ k, long long k_stride,
-            const T* __restrict__ v, long long v_stride, int n_tokens, const int32_t* __restrict__ cu, PlanWs ws, unsigned store_blocks) {
-  if (blockIdx.x >= store_blocks) {
-    const int i = (int)(blockIdx.x - store_blocks);
+            const T* __restrict__ v, long long v_stride, int n_tokens, const int32_t* __restrict__ cu, PlanWs ws) {
+  const int h = blockIdx.y >> 1, which = blockIdx.y & 1;
+  if (h >= c.Hkv) {  // (sequence, head) by (sequence, head)
+    const int cow = (blockIdx.y - 2 * c.Hkv) * gridDim.x + blockIdx.x, step = (gridDim.y - 2 * c.Hkv) * gridDim.x;
     pdl_wait();
     if (!*ws.ok) return;
-    const int old = ws.info[i];
-    if (old < 0) return;
-    const int L = lens[i] - (cu ? cu[i + 1] - cu[i] : 1);
-    const int fresh = table[(size_t)i * c.max_pages + L / c.ps], rows = L % c.ps;
-    const int words = c.d >> 3, sbytes = c.d >> 4;  // 32-bit words of a code row, bytes of a scale row
-    const int per_row = 2 * (words + sbytes);
-    for (int e = threadIdx.x; e < rows * c.Hkv * per_row; e += STORE_THREADS) {
-      const int x = e % per_row, r = e / per_row % rows, h = e / per_row / rows;
-      const uint8_t* a = kv4_group(c, old, h, r >> 4);
-      uint8_t* b = kv4_group(c, fresh, h, r >> 4);
-      const int which = x >= words + sbytes, y = x - which * (words + sbytes);
-      if (y < words) {
-        const int o = (which ? kv4_vc(c.d, r & 15) : kv4_kc(c.d, r & 15)) + 4 * y;
+    for (int task = cow; task < c.n_seqs * c.Hkv; task += step) {
+      const int i = task / c.Hkv, hh = task % c.Hkv;
+      const int old = ws.info[i];
+      if (old < 0) continue;
+      const int L = lens[i] - (cu ? cu[i + 1] - cu[i] : 1), rows = L % c.ps;
+      const int fresh = table[(size_t)i * c.max_pages + L / c.ps];
+      const uint8_t* a = kv4_group(c, old, hh, 0);
+      uint8_t* b = kv4_group(c, fresh, hh, 0);
+      const int row16 = c.d >> 5, group = kv4_group_bytes(c.d);  // 16-byte pieces of a code row
+      // the rows of a section lie side by side: whole pieces of the codes, words of the scales
+#pragma unroll 2
+      for (int e = threadIdx.x; e < rows * 2 * row16; e += STORE_THREADS) {
+        const int r = e / (2 * row16), x = e % (2 * row16);
+        const int o = (r >> 4) * group + (x < row16 ? kv4_kc(c.d, r & 15) + 16 * x : kv4_vc(c.d, r & 15) + 16 * (x - row16));
+        *reinterpret_cast<uint4*>(b + o) = *reinterpret_cast<const uint4*>(a + o);
+      }
+      const int row4 = c.d >> 6;
+      for (int e = threadIdx.x; e < rows * 2 * row4; e += STORE_THREADS) {
+        const int r = e / (2 * row4), x = e % (2 * row4);
+        const int o = (r >> 4) * group + (x < row4 ? kv4_ks(c.d, r & 15) + 4 * x : kv4_vs(c.d, r & 15) + 4 * (x - row4));
         *reinterpret_cast<uint32_t*>(b + o) = *reinterpret_cast<const uint32_t*>(a + o);
-      } else {
-        const int o = (which ? kv4_vs(c.d, r & 15) : kv4_ks(c.d, r & 15)) + y - words;
-        b[o] = a[o];
       }
     }
     return;
   }
-  const int nb = c.d >> 4;
-  const long long idx = (long long)blockIdx.x * STORE_THREADS + threadIdx.x;
-  const int blk = (int)(idx % nb);
-  const long long rest = idx / nb;
-  const int t = (int)(rest % n_tokens), hw = (int)(rest / n_tokens);
-  const bool there = hw < 2 * c.Hkv;
-  const int h = hw >> 1, which = hw & 1;
+  const int lg = c.d == 64 ? 2 : c.d == 128 ? 3 : 4;  // log2 of the blocks of a row
+  const int idx = blockIdx.x * STORE_THREADS + threadIdx.x, blk = idx & ((1 << lg) - 1), t = idx >> lg;
   int i = -1;
   uint2 codes = make_uint2(0u, 0u);
   uint8_t scale = 0;
-  if (there) {
+  if (t < n_tokens) {
     const uint4* src = reinterpret_cast<const uint4*>((which ? v + t * v_stride : k + t * k_stride) + (size_t)h * c.d + blk * 16);
     const uint4 a = src[0], b = src[1];
     const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -322,21 +322,9 @@ k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict_
 }
 
 // ------------------------------------------------------------------ gather
-// One thread per (row, head, block of 16 channels), keys and values: index in the order of the output, which is what
-// most of the bytes are.
+// One thread per (row, head, 8 channels), keys and values: index in the order of the output, which is what most of the
+// bytes are, so that a warp writes 512 bytes side by side.
 constexpr int GATHER_THREADS = 256;
-__device__ __forceinline__ void values16(uint2 codes, uint8_t scale, float up, float* x) {
-  const float s = kv4_unpack_f16(kv4_f16x2_e4m3(scale)).x * up;
-  uint32_t pair[8];
-  kv4_f16_e2m1(codes.x, pair);
-  kv4_f16_e2m1(codes.y, pair + 4);
-#pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const float2 f = kv4_unpack_f16(pair[q]);
-    x[2 * q] = f.x * s;
-    x[2 * q + 1] = f.y * s;
-  }
-}
 template <typename T>
 __device__ __forceinline__ uint32_t pack_two(float a, float b);
 template <>
@@ -352,17 +340,23 @@ __device__ __forceinline__ uint32_t pack_two<__half>(float a, float b) {
   return r;
 }
 template <typename T>
-__device__ __forceinline__ void store16(T* dst, const float* x) {
-  uint4* p = reinterpret_cast<uint4*>(dst);
+__device__ __forceinline__ void put8(T* dst, uint32_t codes, uint8_t scale, float up) {
+  uint32_t pair[4];
+  kv4_f16_e2m1(codes, pair);
+  const float s = kv4_unpack_f16(kv4_f16x2_e4m3(scale)).x * up;
+  float2 f[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    f[q] = kv4_unpack_f16(pair[q]);
+    f[q].x *= s;
+    f[q].y *= s;
+  }
   if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      p[q] = make_uint4(__float_as_uint(x[4 * q]), __float_as_uint(x[4 * q + 1]), __float_as_uint(x[4 * q + 2]), __float_as_uint(x[4 * q + 3]));
+    reinterpret_cast<float4*>(dst)[0] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+    reinterpret_cast<float4*>(dst)[1] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
   } else {
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-      p[q] = make_uint4(pack_two<T>(x[8 * q], x[8 * q + 1]), pack_two<T>(x[8 * q + 2], x[8 * q + 3]),
-                        pack_two<T>(x[8 * q + 4], x[8 * q + 5]), pack_two<T>(x[8 * q + 6], x[8 * q + 7]));
+    *reinterpret_cast<uint4*>(dst) =
+        make_uint4(pack_two<T>(f[0].x, f[0].y), pack_two<T>(f[1].x, f[1].y), pack_two<T>(f[2].x, f[2].y), pack_two<T>(f[3].x, f[3].y));
   }
 }
 
@@ -370,39 +364,34 @@ template <typename T>
 __global__ void __launch_bounds__(GATHER_THREADS)
 k_kv4_gather(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, int n_rows, const int32_t* __restrict__ cu,
              const int32_t* __restrict__ slots, T* __restrict__ k, T* __restrict__ v) {
-  const int nb = c.d >> 4;
-  const long long idx = (long long)blockIdx.x * GATHER_THREADS + threadIdx.x;
-  const int blk = (int)(idx % nb), h = (int)(idx / nb % c.Hkv);
-  const long long r = idx / nb / c.Hkv;
+  const int lg = c.d == 64 ? 3 : c.d == 128 ? 4 : 5;  // log2 of the threads of a row
+  const unsigned idx = blockIdx.x * GATHER_THREADS + threadIdx.x;
+  const int x = (int)(idx & ((1u << lg) - 1u));
+  const unsigned rh = idx >> lg;
+  const int r = (int)(rh / (unsigned)c.Hkv), h = (int)(rh % (unsigned)c.Hkv);
   if (r >= n_rows) return;
-  const int i = kv4_find(cu, c.n_seqs, (int)r);
+  int slot = slots ? slots[r] : 0;
+  const int i = kv4_find(cu, c.n_seqs, r);
   if (i < 0) return;
-  const int slot = slots ? slots[r] : (cu ? (int)r - cu[i] : 0);
-  uint2 kc = make_uint2(0u, 0u), vc = kc;
+  if (!slots && cu) slot = r - cu[i];
+  uint32_t kc = 0, vc = 0;
   uint8_t ks = 0, vs = 0;
   if (slot >= 0 && slot < lens[i] && slot / c.ps < c.max_pages) {
     const int page = table[(size_t)i * c.max_pages + slot / c.ps];
     if (page >= 0 && page < c.n_pages) {
       const int at = slot % c.ps;
       const uint8_t* g = kv4_group(c, page, h, at >> 4);
-      kc = *reinterpret_cast<const uint2*>(g + kv4_kc(c.d, at & 15) + 8 * blk);
-      ks = g[kv4_ks(c.d, at & 15) + blk];
-      vc = *reinterpret_cast<const uint2*>(g + kv4_vc(c.d, at & 15) + 8 * blk);
-      vs = g[kv4_vs(c.d, at & 15) + blk];
-    } else if (blk == 0) {
+      kc = *reinterpret_cast<const uint32_t*>(g + kv4_kc(c.d, at & 15) + 4 * x);
+      ks = g[kv4_ks(c.d, at & 15) + (x >> 1)];
+      vc = *reinterpret_cast<const uint32_t*>(g + kv4_vc(c.d, at & 15) + 4 * x);
+      vs = g[kv4_vs(c.d, at & 15) + (x >> 1)];
+    } else if (x == 0) {
       atomicOr(c.status, IM_KV4_BAD_MAP);
     }
   }
-  const size_t at = ((size_t)r * c.Hkv + h) * c.d + blk * 16;
-  float x[16];
-  if (k) {
-    values16(kc, ks, kv4_pow2(kv4_exp(c.k_exp, h)), x);
-    store16<T>(k + at, x);
-  }
-  if (v) {
-    values16(vc, vs, kv4_pow2(kv4_exp(c.v_exp, h)), x);
-    store16<T>(v + at, x);
-  }
+  const size_t at = (size_t)idx * 8;
+  if (k) put8(k + at, kc, ks, kv4_pow2(kv4_exp(c.k_exp, h)));
+  if (v) put8(v + at, vc, vs, kv4_pow2(kv4_exp(c.v_exp, h)));
 }
 
 // ------------------------------------------------------------------ fork
@@ -511,36 +500,43 @@ k_kv4_scan(Kv4 c, im_kv4_map from, const uint8_t* __restrict__ keep, int keep_st
   }
 }
 
-// A warp writes one group of 16 tokens of one head (18 d bytes side by side) from wherever its tokens were.  Block =
-// (sequence, group), the warps take the heads.
-constexpr int MOVE_THREADS = 256;
+// A warp writes one group of 16 tokens of one head (18 d bytes side by side) from wherever its tokens were.  Block = (sequence,
+// two groups), the warps take (head, group) in turn.  A block is over after two dependent round trips (who
+// moves, the move), and eight of them share an SM; the groups ahead of the first hole have nothing to do.
+constexpr int MOVE_THREADS = 256, MOVE_GROUPS = 2;
 template <int D>
-__global__ void __launch_bounds__(MOVE_THREADS) k_kv4_move(Kv4 c, const int32_t* __restrict__ table, PlanWs ws, int groups) {
+__global__ void __launch_bounds__(MOVE_THREADS) k_kv4_move(Kv4 c, const int32_t* __restrict__ table, PlanWs ws, int blocks) {
   constexpr int ROW16 = D / 32;            // 16-byte pieces of a code row
   constexpr int CODES = 2 * 16 * ROW16;    // of a group: keys, then values
-  const int i = blockIdx.x / groups, lane = threadIdx.x & 31;
+  const int i = blockIdx.x / blocks, base = (blockIdx.x % blocks) * (16 * MOVE_GROUPS), lane = threadIdx.x & 31;
   pdl_wait();
-  if (!*ws.ok) return;
-  const int cnt = ws.cnt[i], first = ws.info[i] * c.ps;
-  const int j0 = first + (blockIdx.x % groups) * 16;
-  if (j0 >= cnt) return;
-  const int rows = min(16, cnt - j0);
-  const int page = table[(size_t)i * c.max_pages + j0 / c.ps];
-  const int src = lane < rows ? ws.src[(size_t)i * ws.cap + j0 + lane] : 0;  // lane r: where row r was
-  for (int h = threadIdx.x >> 5; h < c.Hkv; h += MOVE_THREADS / 32) {
-    uint8_t* g = kv4_group(c, page, h, (j0 % c.ps) >> 4);
+  // every lane: where row (lane % 16) of either group was, and the groups' pages; asked for at once, used if they are valid
+  const int ok = *ws.ok, cnt = ws.cnt[i], first = ws.info[i] * c.ps;
+  int src[MOVE_GROUPS], page[MOVE_GROUPS];
+#pragma unroll
+  for (int m = 0; m < MOVE_GROUPS; ++m) {
+    const int j = base + 16 * m + (lane & 15);
+    src[m] = j < ws.cap ? ws.src[(size_t)i * ws.cap + j] : 0;
+    page[m] = j < ws.cap ? table[(size_t)i * c.max_pages + j / c.ps] : 0;
+  }
+  if (!ok || base + 16 * MOVE_GROUPS <= first || base >= cnt) return;
+  for (int task = threadIdx.x >> 5; task < MOVE_GROUPS * c.Hkv; task += MOVE_THREADS / 32) {
+    const int m = task / c.Hkv, h = task % c.Hkv, j0 = base + 16 * m;
+    if (j0 < first || j0 >= cnt) continue;
+    const int rows = min(16, cnt - j0);
+    const int from = (lane & 15) < rows ? (m ? src[1] : src[0]) : 0;
+    uint8_t* g = kv4_group(c, m ? page[1] : page[0], h, (j0 % c.ps) >> 4);
     uint4 code[CODES / 32];
 #pragma unroll
     for (int q = 0; q < CODES / 32; ++q) {
       const int e = q * 32 + lane, which = e / (16 * ROW16), r = e / ROW16 % 16, x = e % ROW16;
-      const int s = __shfl_sync(0xffffffffu, src, r);
+      const int s = __shfl_sync(0xffffffffu, from, r);
       const uint8_t* a = kv4_group(c, s / c.ps, h, (s % c.ps) >> 4) + (which ? kv4_vc(D, s & 15) : kv4_kc(D, s & 15)) + 16 * x;
       code[q] = r < rows ? *reinterpret_cast<const uint4*>(a) : make_uint4(0u, 0u, 0u, 0u);
     }
     // scales: lane = (which, row), D / 16 bytes each
     const int which = lane >> 4, r = lane & 15;
-    const int s = __shfl_sync(0xffffffffu, src, r);
-    const uint8_t* a = kv4_group(c, s / c.ps, h, (s % c.ps) >> 4) + (which ? kv4_vs(D, s & 15) : kv4_ks(D, s & 15));
+    const uint8_t* a = kv4_group(c, from / c.ps, h, (from % c.ps) >> 4) + (which ? kv4_vs(D, from & 15) : kv4_ks(D, from & 15));
     uint32_t scale[D / 64];
 #pragma unroll
     for (int q = 0; q < D / 64; ++q) scale[q] = r < rows ? reinterpret_cast<const uint32_t*>(a)[q] : 0u;
@@ -614,6 +610,24 @@ int check_maps(const Kv4& c, const im_kv4_map* from, const im_kv4_map* to, const
     return kv4_fail(IM_ERR_ARG, fn, "`to` must be `from` or not overlap it");
   return IM_OK;
 }
+// One CTA for pools it counts in a few rounds (no cluster barriers), else a cluster.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_plan(void (*kernel)(KArgs...), const Kv4& c, cudaStream_t s, bool dependent, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  const int ctas = c.n_pages <= PLAN_ONE_CTA_PAGES ? 1 : PLAN_CTAS;
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(PLAN_THREADS);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = dependent ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, (KArgs)args...);
+}
 int launched(cudaError_t e) { return e == cudaSuccess ? IM_OK : im_fail_message(IM_ERR_CUDA, cudaGetErrorString(e)); }
 
 }  // namespace
@@ -679,18 +693,19 @@ extern "C" int im_kv4_append(const im_kv4* cache, const im_kv4_map* from, const 
   PlanWs ws;
   if (!workspace || ((uintptr_t)workspace & 255) || append_workspace(c, n_tokens, (uint8_t*)workspace, &ws) > workspace_bytes)
     return kv4_fail(IM_ERR_CAPACITY, fn, "workspace missing, misaligned or too small");
-  const long long blocks = ((long long)n_tokens * 2 * c.Hkv * (c.d / 16) + STORE_THREADS - 1) / STORE_THREADS;
-  if (blocks + c.n_seqs > 0x7fffffffll) return kv4_fail(IM_ERR_ARG, fn, "too many tokens in one call");
+  if ((long long)n_tokens * (c.d / 16) > 0x7fffff00ll) return kv4_fail(IM_ERR_ARG, fn, "too many tokens in one call");
   cudaStream_t s = (cudaStream_t)cuda_stream;
-  cudaError_t e = kv4_launch(k_kv4_plan<PLAN_APPEND>, dim3(PLAN_CTAS), PLAN_THREADS, 0, s, false, c, *from, *to, cu_new, n_tokens, ws);
+  cudaError_t e = launch_plan(k_kv4_plan<PLAN_APPEND>, c, s, false, c, *from, *to, cu_new, n_tokens, ws);
   if (e == cudaSuccess && n_tokens > 0) {
-    const dim3 grid((unsigned)(blocks + c.n_seqs));
+    const int x = (n_tokens * (c.d / 16) + STORE_THREADS - 1) / STORE_THREADS;
+    const long long tasks = (long long)c.n_seqs * c.Hkv, copiers = tasks < 592 ? tasks : 592;  // (four blocks per SM)
+    const dim3 grid(x, 2 * c.Hkv + (int)((copiers + x - 1) / x));
     if (dtype == IM_BF16)
       e = kv4_launch(k_kv4_store<bf16>, grid, STORE_THREADS, 0, s, true, c, to->table, to->lens, (const bf16*)k, k_stride, (const bf16*)v,
-                     v_stride, n_tokens, cu_new, ws, (unsigned)blocks);
+                     v_stride, n_tokens, cu_new, ws);
     else
       e = kv4_launch(k_kv4_store<__half>, grid, STORE_THREADS, 0, s, true, c, to->table, to->lens, (const __half*)k, k_stride,
-                     (const __half*)v, v_stride, n_tokens, cu_new, ws, (unsigned)blocks);
+                     (const __half*)v, v_stride, n_tokens, cu_new, ws);
   }
   return launched(e);
 }
@@ -705,8 +720,8 @@ extern "C" int im_kv4_gather(const im_kv4* cache, const im_kv4_map* map, int n_r
   if (n_rows < 0 || (!cu_rows && n_rows != c.n_seqs)) return kv4_fail(IM_ERR_ARG, fn, "bad row count");
   if (dtype != IM_BF16 && dtype != IM_F16 && dtype != IM_F32) return kv4_fail(IM_ERR_ARG, fn, "unknown dtype");
   if ((!k && !v && n_rows) || (((uintptr_t)k | (uintptr_t)v) & 15)) return kv4_fail(IM_ERR_ARG, fn, "null or misaligned output");
-  const long long blocks = ((long long)n_rows * c.Hkv * (c.d / 16) + GATHER_THREADS - 1) / GATHER_THREADS;
-  if (blocks > 0x7fffffffll) return kv4_fail(IM_ERR_ARG, fn, "too many rows in one call");
+  const long long blocks = ((long long)n_rows * c.Hkv * (c.d / 8) + GATHER_THREADS - 1) / GATHER_THREADS;
+  if (blocks > 0xffffffffll / GATHER_THREADS) return kv4_fail(IM_ERR_ARG, fn, "too many rows in one call");
   if (!blocks) return IM_OK;
   const dim3 grid((unsigned)blocks);
   cudaStream_t s = (cudaStream_t)cuda_stream;
@@ -749,16 +764,16 @@ extern "C" int im_kv4_compact(const im_kv4* cache, const im_kv4_map* from, const
   PlanWs ws;
   if (!workspace || ((uintptr_t)workspace & 255) || compact_workspace(c, keep_stride, (uint8_t*)workspace, &ws) > workspace_bytes)
     return kv4_fail(IM_ERR_CAPACITY, fn, "workspace missing, misaligned or too small");
-  const int groups = (ws.cap + 15) / 16;
-  if ((long long)groups * c.n_seqs > 0x7fffffffll) return kv4_fail(IM_ERR_ARG, fn, "map too large");
+  const int blocks = (ws.cap + 16 * MOVE_GROUPS - 1) / (16 * MOVE_GROUPS);
+  if ((long long)blocks * c.n_seqs > 0x7fffffffll) return kv4_fail(IM_ERR_ARG, fn, "map too large");
   cudaStream_t s = (cudaStream_t)cuda_stream;
   cudaError_t e = kv4_launch(k_kv4_scan, dim3(c.n_seqs), SCAN_THREADS, 0, s, false, c, *from, keep, keep_stride, ws);
-  if (e == cudaSuccess) e = kv4_launch(k_kv4_plan<PLAN_COMPACT>, dim3(PLAN_CTAS), PLAN_THREADS, 0, s, true, c, *from, *to, (const int32_t*)nullptr, 0, ws);
+  if (e == cudaSuccess) e = launch_plan(k_kv4_plan<PLAN_COMPACT>, c, s, true, c, *from, *to, (const int32_t*)nullptr, 0, ws);
   if (e == cudaSuccess) {
-    const dim3 grid((unsigned)(groups * c.n_seqs));
-    if (c.d == 64) e = kv4_launch(k_kv4_move<64>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, groups);
-    else if (c.d == 128) e = kv4_launch(k_kv4_move<128>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, groups);
-    else e = kv4_launch(k_kv4_move<256>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, groups);
+    const dim3 grid((unsigned)(blocks * c.n_seqs));
+    if (c.d == 64) e = kv4_launch(k_kv4_move<64>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, blocks);
+    else if (c.d == 128) e = kv4_launch(k_kv4_move<128>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, blocks);
+    else e = kv4_launch(k_kv4_move<256>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, blocks);
   }
   return launched(e);
 }

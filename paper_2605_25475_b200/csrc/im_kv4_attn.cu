@@ -590,66 +590,101 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
 }
 
 // Joins the partial results of the items that several warps share, and writes the rows that see nothing.  Block = (query token,
-// KV head), a warp per row.
+// query head); its warps take the partial results in turn, so that all of them are asked for at once.
 template <int D, int NT, typename OutT>
 __global__ void __launch_bounds__(MERGE_THREADS) k_kv4_merge(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
-  constexpr int ROWS = 8 * NT, CH = D / 32;
-  const int t = blockIdx.x, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int ROWS = 8 * NT, CH = D / 32, WARPS = MERGE_THREADS / 32;
+  __shared__ float s_acc[WARPS][D], s_m[WARPS], s_l[WARPS];
+  const int t = blockIdx.x, head = blockIdx.y, h = head / a.G, j = head % a.G, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int i = kv4_find(a.cu, a.c.n_seqs, t);
   if (i < 0) return;
   const Seq s = seq_of<ROWS>(a, i);
   const float vup = kv4_pow2(kv4_exp(a.c.v_exp, h));
+  const int r = (t - s.first) * a.G + j;
+  float acc[CH], total = 0.f, m = NO_MAX;
+#pragma unroll
+  for (int k = 0; k < CH; ++k) acc[k] = 0.f;
   pdl_wait();
-  const Deal deal = *a.ws.deal;
-  const long long cum = a.ws.cum[i];
-  auto worker_of = [&](long long x) {
-    return x < deal.rest * (deal.q + 1) ? x / (deal.q + 1) : deal.rest + (x - deal.rest * (deal.q + 1)) / deal.q;
-  };
-  for (int j = warp; j < a.G; j += MERGE_THREADS / 32) {
-    const int r = (t - s.first) * a.G + j;
-    const size_t at = (size_t)t * a.H + h * a.G + j;
-    float acc[CH], total = 0.f, m = NO_MAX;
+  if (s.tiles) {
+    const Deal deal = *a.ws.deal;
+    const long long base = a.ws.cum[i] + ((long long)h * s.rb + r / ROWS) * s.tiles;
+    auto worker_of = [&](long long x) {
+      const long long big = deal.rest * (deal.q + 1);
+      if (((big | x) >> 31) == 0) {
+        const unsigned q = (unsigned)deal.q;
+        return x < big ? (int)((unsigned)x / (q + 1)) : (int)deal.rest + (int)((unsigned)(x - big) / q);
+      }
+      return (int)(x < big ? x / (deal.q + 1) : deal.rest + (x - big) / deal.q);
+    };
+    const int w0 = worker_of(base), w1 = worker_of(base + s.tiles - 1);
+    if (w0 == w1) return;  // written where it was computed
+    // worker w's result: its run began ahead of the item, but for the first one's
+    const float* part = a.ws.part + (size_t)(r % ROWS) * (D + 4);
+    for (int b = w0 + warp * 32; b <= w1; b += MERGE_THREADS) {
+      const int mine = b + lane;
+      float2 ml = make_float2(NO_MAX, 0.f);
+      if (mine <= w1) ml = *reinterpret_cast<const float2*>(part + (size_t)(2 * mine + (mine == w0 ? 1 : 0)) * (ROWS * (D + 4)) + D);
+      float mb = ml.x;
 #pragma unroll
-    for (int k = 0; k < CH; ++k) acc[k] = 0.f;
-    if (s.tiles) {
-      const long long base = cum + ((long long)h * s.rb + r / ROWS) * s.tiles;
-      const long long w0 = worker_of(base), w1 = worker_of(base + s.tiles - 1);
-      if (w0 == w1) continue;  // written where it was computed
-      auto slot = [&](long long w) {
-        const long long start = w * deal.q + min(w, deal.rest);
-        return a.ws.part + ((size_t)(2 * w + (start <= base ? 1 : 0)) * ROWS + r % ROWS) * (D + 4);
-      };
-      for (long long w = w0 + lane; w <= w1; w += 32) m = fmaxf(m, slot(w)[D]);
+      for (int x = 1; x < 32; x <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, x));
+      mb = fmaxf(mb, m);
+      const float corr = ex2(m - mb), e = ex2(ml.x - mb);
+      m = mb;
+      float le = ml.y * e;
 #pragma unroll
-      for (int x = 1; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-#pragma unroll 4
-      for (long long w = w0; w <= w1; ++w) {
-        const float* p = slot(w);
-        const float2 ml = *reinterpret_cast<const float2*>(p + D);
-        const float e = ex2(ml.x - m);
-        total = fmaf(ml.y, e, total);
+      for (int x = 1; x < 32; x <<= 1) le += __shfl_xor_sync(0xffffffffu, le, x);
+      total = fmaf(total, corr, le);
+#pragma unroll
+      for (int k = 0; k < CH; ++k) acc[k] *= corr;
+      const int n = min(32, w1 + 1 - b);
+#pragma unroll 8
+      for (int x = 0; x < n; ++x) {
+        const int w = b + x;
+        const float by = __shfl_sync(0xffffffffu, e, x);
+        const float* p = part + (size_t)(2 * w + (w == w0 ? 1 : 0)) * (ROWS * (D + 4));
         if constexpr (CH == 2) {
           const float2 v = *reinterpret_cast<const float2*>(p + 2 * lane);
-          acc[0] = fmaf(v.x, e, acc[0]), acc[1] = fmaf(v.y, e, acc[1]);
+          acc[0] = fmaf(v.x, by, acc[0]), acc[1] = fmaf(v.y, by, acc[1]);
         } else {
 #pragma unroll
           for (int k = 0; k < CH; k += 4) {
             const float4 v = *reinterpret_cast<const float4*>(p + CH * lane + k);
-            acc[k] = fmaf(v.x, e, acc[k]), acc[k + 1] = fmaf(v.y, e, acc[k + 1]);
-            acc[k + 2] = fmaf(v.z, e, acc[k + 2]), acc[k + 3] = fmaf(v.w, e, acc[k + 3]);
+            acc[k] = fmaf(v.x, by, acc[k]), acc[k + 1] = fmaf(v.y, by, acc[k + 1]);
+            acc[k + 2] = fmaf(v.z, by, acc[k + 2]), acc[k + 3] = fmaf(v.w, by, acc[k + 3]);
           }
         }
       }
     }
-    const float inv = total == 0.f ? 0.f : vup / total;
-    OutT* dst = out + at * D + CH * lane;
+    if (w1 - w0 >= 32) {  // (the same for the whole block)
 #pragma unroll
-    for (int k = 0; k < CH; k += 2) {
-      if constexpr (sizeof(OutT) == 2) *reinterpret_cast<uint32_t*>(dst + k) = pack_two(dst, acc[k] * inv, acc[k + 1] * inv);
-      else *reinterpret_cast<float2*>(dst + k) = make_float2(acc[k] * inv, acc[k + 1] * inv);
+      for (int k = 0; k < CH; ++k) s_acc[warp][CH * lane + k] = acc[k];
+      if (lane == 0) s_m[warp] = m, s_l[warp] = total;
+      __syncthreads();
+      if (warp) return;
+#pragma unroll
+      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_m[w]);
+      total = 0.f;
+#pragma unroll
+      for (int k = 0; k < CH; ++k) acc[k] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float by = ex2(s_m[w] - m);
+        total = fmaf(s_l[w], by, total);
+#pragma unroll
+        for (int k = 0; k < CH; ++k) acc[k] = fmaf(s_acc[w][CH * lane + k], by, acc[k]);
+      }
     }
-    if (lse && lane == 0) lse[at] = total == 0.f ? NEG_INF : (m + log2f(total)) * LN2;
   }
+  if (warp) return;
+  const size_t at = (size_t)t * a.H + head;
+  const float inv = total == 0.f ? 0.f : vup / total;
+  OutT* dst = out + at * D + CH * lane;
+#pragma unroll
+  for (int k = 0; k < CH; k += 2) {
+    if constexpr (sizeof(OutT) == 2) *reinterpret_cast<uint32_t*>(dst + k) = pack_two(dst, acc[k] * inv, acc[k + 1] * inv);
+    else *reinterpret_cast<float2*>(dst + k) = make_float2(acc[k] * inv, acc[k + 1] * inv);
+  }
+  if (lse && lane == 0) lse[at] = total == 0.f ? NEG_INF : (m + log2f(total)) * LN2;
 }
 
 int sm_count() {
@@ -686,7 +721,7 @@ cudaError_t launch(const AttnArgs& a, const void* q, void* out, float* lse, int 
     *done = true;
   }
   cudaError_t e = kv4_launch(k_kv4_stream<D, NT, TWO, T, OutT>, dim3(grid), warps_of(D, NT) * 32, smem, s, false, a, (const T*)q, (OutT*)out, lse);
-  if (e == cudaSuccess) e = kv4_launch(k_kv4_merge<D, NT, OutT>, dim3(a.n_tokens, a.c.Hkv), MERGE_THREADS, 0, s, true, a, (OutT*)out, lse);
+  if (e == cudaSuccess) e = kv4_launch(k_kv4_merge<D, NT, OutT>, dim3(a.n_tokens, a.H), MERGE_THREADS, 0, s, true, a, (OutT*)out, lse);
   return e;
 }
 
