@@ -495,8 +495,8 @@ typedef struct im_kv4_map {
 /* Bytes of one page; 0 if the sizes are not supported. */
 size_t im_kv4_page_bytes(int n_kv_heads, int head_dim, int page_size);
 
-/* Bytes of workspace for a call: op 0 im_kv4_append (n = n_tokens), 1 im_kv4_attention (n = n_tokens), 2 im_kv4_compact
- * (n = keep_stride; n_q_heads is read by op 1 alone).  0 if the arguments are invalid. */
+/* Bytes of workspace for a call: op 0 im_kv4_append (n = n_tokens), 1 im_kv4_attention (n = max_q, or 1 without cu_q; the one op
+ * that reads n_q_heads), 2 im_kv4_compact (n = keep_stride).  0 if the arguments are invalid. */
 size_t im_kv4_workspace_bytes(const im_kv4* cache, int op, int n, int n_q_heads);
 
 /*

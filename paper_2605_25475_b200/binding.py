@@ -660,12 +660,13 @@ class KV4Cache:
         return m
 
     def _call(self, fn, *args):
+        # (the raw handles: a torch Stream object costs 3 us, half of a small call)
         d = self.device.index
-        if torch.cuda.current_device() == d:
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        if torch._C._cuda_getDevice() == d:
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(d))
         else:
             with torch.cuda.device(d):
-                rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+                rc = fn(*args, torch._C._cuda_getCurrentRawStream(d))
         if rc != IM_OK:
             _check(rc)
 
@@ -679,15 +680,21 @@ class KV4Cache:
             if len(self._ws_bytes) >= 256:
                 self._ws_bytes.clear()
             self._ws_bytes[op, n, heads] = nbytes
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device), nbytes
+        return self.pool.new_empty(nbytes), nbytes
 
     def _rows_of(self, t, heads, name):
         """A [n, heads, head_dim] tensor whose tokens may be strided (a slice of a fused projection): its token stride."""
-        if t.device != self.device or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.stride(2) != 1 or \
-                (heads > 1 and t.stride(1) != self.head_dim) or (t.shape[0] > 1 and t.stride(0) < heads * self.head_dim):
-            raise ValueError(f"{name}: need [tokens, {heads}, {self.head_dim}] on {self.device}, dense within a token, got "
-                             f"{tuple(t.shape)} {t.stride()} {t.device}")
-        return t.stride(0) if t.shape[0] > 1 else 0
+        d = self.head_dim
+        if t.device == self.device and t.dim() == 3:
+            n, h, w = t.shape
+            if h == heads and w == d:
+                if t.is_contiguous():
+                    return 0
+                a, b, c = t.stride()
+                if c == 1 and (b == d or h == 1) and (a >= h * d or n <= 1):
+                    return a if n > 1 else 0
+        raise ValueError(f"{name}: need [tokens, {heads}, {d}] on {self.device}, dense within a token, got {tuple(t.shape)} {t.stride()} "
+                         f"{t.device}")
 
     def _starts(self, cu, n, what):
         """cu (int32 [n_seqs + 1] on the device) or None: one of each sequence."""
@@ -719,18 +726,18 @@ class KV4Cache:
         """Attention of q bf16 / f16 [n_tokens, n_q_heads, head_dim] over the cache: tokens cu_q[i] .. cu_q[i + 1] - 1 see
         sequence i, whose last tokens they are if causal.  max_q: the largest number of them (it chooses the kernels).
         Returns out (q's type, or float32), with return_lse also the log of the softmax's sum, float32 [n_tokens, n_q_heads]."""
-        n, H = q.shape[0], q.shape[1]
+        if q.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("q: bf16 or f16 [tokens, heads, head_dim]")
+        n, H, _ = q.shape
         qs = self._rows_of(q, H, "q")
-        if q.dtype not in (torch.bfloat16, torch.float16):
-            raise ValueError("q: bf16 or f16")
         dtype = torch.float32 if out_f32 else q.dtype
         if out is None:
-            out = torch.empty((n, H, self.head_dim), dtype=dtype, device=self.device)
+            out = q.new_empty((n, H, self.head_dim)) if not out_f32 else torch.empty((n, H, self.head_dim), dtype=dtype, device=self.device)
         elif out.device != self.device or out.dtype != dtype or tuple(out.shape) != (n, H, self.head_dim) or not out.is_contiguous():
             raise ValueError(f"out: need a contiguous {dtype} tensor {(n, H, self.head_dim)} on {self.device}")
         lse = torch.empty((n, H), dtype=torch.float32, device=self.device) if return_lse else None
         m = self.map if map is None else self._check_map(map)
-        ws, nbytes = self._workspace(1, n, H)
+        ws, nbytes = self._workspace(1, 1 if cu_q is None else max_q, H)
         self._call(_lib.im_kv4_attention, self._p, m._p, _DTYPE_IDS[q.dtype], q.data_ptr(), qs, n, self._starts(cu_q, n, "attend"),
                    max_q, H, softmax_scale, 1 if causal else 0, out.data_ptr(), 1 if out_f32 else 0, _ptr(lse), ws.data_ptr(), nbytes)
         return (out, lse) if return_lse else out

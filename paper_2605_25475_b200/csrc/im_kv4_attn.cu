@@ -3,10 +3,7 @@
 // k_kv4_stream: the few query rows of a (sequence, KV head) against its entries.  The floor is one pass over the cache,
 // 1.125 head_dim bytes per entry and KV head; next to it stands the work of unpacking: every code has to become an f16 in a
 // register before a tensor core takes it, two per conversion instruction and two per multiplication with the block's scale.
-//   split    The entries of all (sequence, KV head, row block) items form one line of tiles of 32; every warp of a
-//            persistent grid gets an equal run of it, whatever the lengths are (they are known to the device alone).  A run that
-//            does not cover an item writes (sum of p v, reference maximum, sum of p) to the workspace, and k_kv4_merge adds those up
-//            in order of the warps: results do not depend on timing.
+//   split    The line of tiles (im_kv4_attn.cuh) in tiles of 32 entries; the workers are the warps of a persistent grid.
 //   copies   Each warp has a ring of tiles of its own in shared memory, filled by one bulk copy per tile: the 16-token groups
 //            of a page lie side by side with keys, values and scales.  No barrier but the warp's own.
 //   scores   S^T = K Q^T with mma.m16n8k16: 16 entries on M, 8 rows on N.  The contraction's order is free, so a lane takes
@@ -20,44 +17,16 @@
 //            outputs take P as two f16 terms (2^-22), bf16 outputs one (2^-12, an eighth of their own step).
 #include <math.h>
 
-#include <type_traits>
-
-#include "im_kv4.cuh"
+#include "im_kv4_attn.cuh"
 
 namespace {
 
-constexpr float NEG_INF = -__builtin_huge_valf();
-constexpr float NO_MAX = -1e30f;         // reference maximum of a row that has seen nothing
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int TILE = 32;                 // entries per tile: two groups
-constexpr int RING_BYTES = 221184;       // shared memory of a CTA's rings
-constexpr int MERGE_THREADS = 128;
+constexpr int TILE = 32;            // entries per tile: two groups
+constexpr int RING_BYTES = 221184;  // shared memory of a CTA's rings
 
 constexpr int warps_of(int d, int nt) { return d == 256 ? (nt == 1 ? 12 : 8) : nt == 1 ? 16 : 12; }
 constexpr int stages_of(int d, int nt) { return RING_BYTES / (warps_of(d, nt) * 2 * kv4_group_bytes(d)); }
 
-// how a call's tiles are dealt to the warps (written by CTA 0 of k_kv4_stream for k_kv4_merge)
-struct Deal {
-  long long q, rest;  // the first `rest` workers get q + 1 tiles, the others q
-};
-struct AttnWs {
-  Deal* deal;
-  long long* cum;  // [n_seqs] tiles ahead of the sequence
-  float* part;     // [2 * workers][8 NT][D + 2]
-};
-
-struct AttnArgs {
-  Kv4 c;
-  const int32_t* table;
-  const int32_t* lens;
-  const int32_t* cu;
-  long long q_stride;
-  int n_tokens, H, G, causal;
-  float scale;
-  AttnWs ws;
-};
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   for (uint32_t it = 0; it < IM_WAIT_LIMIT; ++it) {
     uint32_t done;
@@ -72,72 +41,22 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   }
   return false;
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
 __device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the first step of a sum: c = a b
+__device__ __forceinline__ void mma_f16_first(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float2 two_of(const bf16*, uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
-__device__ __forceinline__ uint32_t pack_two(const bf16*, float a, float b) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
-}
-__device__ __forceinline__ uint32_t pack_two(const __half*, float a, float b) { return pack_f16(a, b); }
-
-// query tokens of sequence i, clipped to the tensors
-__device__ __forceinline__ void queries_of(const AttnArgs& a, int i, int* first, int* count) {
-  if (!a.cu) {
-    *first = i;
-    *count = 1;
-    return;
-  }
-  const int s = max(0, min(a.n_tokens, a.cu[i])), e = max(s, min(a.n_tokens, a.cu[i + 1]));
-  *first = s;
-  *count = e - s;
-}
-__device__ __forceinline__ int length_of(const AttnArgs& a, int i) {
-  return (int)max(0ll, min((long long)a.lens[i], (long long)a.c.max_pages * a.c.ps));
-}
-
-// the line of tiles: sequence-major, then KV head, then row block
-struct Seq {
-  int L, first, nq, tiles, rb;  // rb: row blocks
-};
-template <int ROWS>
-__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int i) {
-  Seq s;
-  s.L = length_of(a, i);
-  queries_of(a, i, &s.first, &s.nq);
-  s.rb = (int)(((long long)s.nq * a.G + ROWS - 1) / ROWS);
-  s.tiles = s.nq ? (s.L + TILE - 1) / TILE : 0;
-  return s;
-}
-__device__ __forceinline__ long long work_of(const AttnArgs& a, const Seq& s) { return (long long)s.tiles * s.rb * a.c.Hkv; }
 
 template <int D, int NT, bool TWO, typename T, typename OutT>
 __global__ void __launch_bounds__(warps_of(D, NT) * 32, 1)
@@ -152,129 +71,82 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
   const Kv4& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, cq = lane & 3;
   pdl_release();
-  // ---- the line of tiles: every CTA adds the sequences up for itself
-  const int per = (c.n_seqs + THREADS - 1) / THREADS;
-  {
-    long long mine = 0;
-    for (int i = tid * per; i < min(c.n_seqs, tid * per + per); ++i) mine += work_of(a, seq_of<ROWS>(a, i));
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += u;
-    }
-    if (lane == 31) s_scan[warp] = incl;
-    if (lane < STAGES) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&s_bar[warp][lane])));
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();
-    long long before = 0;
-    for (int w = 0; w < warp; ++w) before += s_scan[w];
-    s_cum[tid] = before + incl - mine;
-    if (tid == THREADS - 1) s_cum[THREADS] = before + incl;
-    __syncthreads();
-  }
-  const long long total = s_cum[THREADS];
-  const int workers = (int)min((long long)gridDim.x * WARPS, max(1ll, total));
-  const long long quo = total / workers, rest = total % workers;
-  if (blockIdx.x == 0) {
-    if (tid == 0) *a.ws.deal = {quo, rest};
-    long long at = s_cum[tid];
-    for (int i = tid * per; i < min(c.n_seqs, tid * per + per); ++i) {
-      a.ws.cum[i] = at;
-      at += work_of(a, seq_of<ROWS>(a, i));
-    }
-  }
+  if (lane < STAGES) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&s_bar[warp][lane])));
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  int workers, per;
+  const Deal deal = deal_line<ROWS, TILE, THREADS>(a, s_cum, s_scan, (long long)gridDim.x * WARPS, &workers, &per);
   const int worker = warp * gridDim.x + blockIdx.x;  // neighbours in the line sit on different SMs
   if (worker >= workers) return;
-  const long long t0 = worker * quo + min((long long)worker, rest), t1 = t0 + quo + (worker < rest ? 1 : 0);
+  const long long t0 = worker * deal.q + min((long long)worker, deal.rest), t1 = t0 + deal.q + (worker < deal.rest ? 1 : 0);
   if (t0 >= t1) return;
-  // ---- where the run starts
-  int i0;
   long long off;
-  {
-    int lo = 0, hi = THREADS;  // s_cum[lo] <= t0 < s_cum[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s_cum[mid] <= t0) lo = mid;
-      else hi = mid;
-    }
-    i0 = lo * per;
-    off = t0 - s_cum[lo];
-    while (true) {
-      const long long w = work_of(a, seq_of<ROWS>(a, i0));
-      if (off < w) break;
-      off -= w;
-      ++i0;
-    }
-  }
-  // ---- the copies' side: sequence pi, item (head, row block) of it, tile pt of its tiles
-  int pi = i0, p_item, p_tile;
-  Seq ps_ = seq_of<ROWS>(a, i0);
-  p_item = (int)(off / ps_.tiles);
-  p_tile = (int)(off % ps_.tiles);
+  const int i0 = find_tile<ROWS, TILE, THREADS>(a, s_cum, per, t0, &off);
+  // ---- the copies' side: sequence pi, KV head ph, row block pr, tile p_tile
+  const Seq first = seq_of<ROWS, TILE>(a, i0);
+  const int item0 = (int)(off / first.tiles), tile0 = (int)(off % first.tiles);
+  Seq sq = first;
+  int pi = i0, ph = item0 / first.rb, pr = item0 % first.rb, p_tile = tile0;
   int left = (int)(t1 - t0);           // tiles still to be requested
-  int win_base = -1, win = 0;          // lane j: page of tile win_base + j (page_size 16: of group 2 win_base + j)
-  const int win_tiles = c.ps == 16 ? 16 : 32;
+  int win_base = 0, win_end = 0, win = 0;  // lane j: page of tile win_base + j (page_size 16: of group 2 win_base + j)
   uint32_t bad = 0;                    // bit 2 s + k: group k of stage s has no page
   uint8_t* ring = s_ring + warp * (STAGES * STAGE);
   const uint32_t bar0 = smem_u32(&s_bar[warp][0]), ring0 = smem_u32(ring);
+  const size_t head_bytes = (size_t)(c.ps >> 4) * GROUP, page_bytes = head_bytes * c.Hkv;
   auto request = [&](int s) {
-    const int h = p_item / ps_.rb;
-    if (win_base < 0 || p_tile >= win_base + win_tiles || p_tile < win_base) {
+    if (p_tile >= win_end) {
+      const int e = c.ps == 16 ? 2 * p_tile + lane : (int)(((long long)(p_tile + lane) * TILE) / c.ps);
+      win = (long long)e * c.ps < sq.L ? a.table[(size_t)pi * c.max_pages + e] : -1;
       win_base = p_tile;
-      const int e = c.ps == 16 ? 2 * win_base + lane : (int)(((long long)(win_base + lane) * TILE) / c.ps);
-      const int pages = (ps_.L + c.ps - 1) / c.ps;
-      win = e < pages ? a.table[(size_t)pi * c.max_pages + e] : -1;
+      win_end = p_tile + (c.ps == 16 ? 16 : 32);
     }
     const uint32_t bar = bar0 + 8 * s, dst = ring0 + s * STAGE;
+    const uint8_t* src = c.pool + ph * head_bytes;
     bad &= ~(3u << (2 * s));
     if (c.ps == 16) {
       const int a0 = __shfl_sync(0xffffffffu, win, 2 * (p_tile - win_base)), a1 = __shfl_sync(0xffffffffu, win, 2 * (p_tile - win_base) + 1);
-      const bool ok0 = a0 >= 0 && a0 < c.n_pages, ok1 = a1 >= 0 && a1 < c.n_pages;
+      const bool ok0 = (unsigned)a0 < (unsigned)c.n_pages, ok1 = (unsigned)a1 < (unsigned)c.n_pages;
       bad |= ((ok0 ? 0u : 1u) | (ok1 ? 0u : 2u)) << (2 * s);
       if (lane == 0) {
-        if (!ok0 || (!ok1 && p_tile * TILE + 16 < ps_.L)) atomicOr(c.status, IM_KV4_BAD_MAP);
+        if (!ok0 || (!ok1 && p_tile * TILE + 16 < sq.L)) atomicOr(c.status, IM_KV4_BAD_MAP);
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)((ok0 + ok1) * GROUP)) : "memory");
-        if (ok0) bulk_load(dst, kv4_group(c, a0, h, 0), GROUP, bar);
-        if (ok1) bulk_load(dst + GROUP, kv4_group(c, a1, h, 0), GROUP, bar);
+        if (ok0) bulk_load(dst, src + a0 * page_bytes, GROUP, bar);
+        if (ok1) bulk_load(dst + GROUP, src + a1 * page_bytes, GROUP, bar);
       }
     } else {
       const int page = __shfl_sync(0xffffffffu, win, p_tile - win_base);
-      const bool ok = page >= 0 && page < c.n_pages;
-      bad |= (ok ? 0u : 3u) << (2 * s);
+      const bool ok = (unsigned)page < (unsigned)c.n_pages;
+      if (!ok) bad |= 3u << (2 * s);
       if (lane == 0) {
         if (!ok) atomicOr(c.status, IM_KV4_BAD_MAP);
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)(ok ? STAGE : 0)) : "memory");
-        if (ok) bulk_load(dst, kv4_group(c, page, h, (p_tile * TILE & (c.ps - 1)) >> 4), STAGE, bar);
-      }
-    }
-    if (++p_tile == ps_.tiles) {
-      p_tile = 0;
-      win_base = -1;
-      if (++p_item == ps_.rb * c.Hkv && left > 1) {
-        p_item = 0;
-        do ps_ = seq_of<ROWS>(a, ++pi);
-        while (ps_.tiles == 0);  // (there is work ahead: left > 1)
+        if (ok) bulk_load(dst, src + page * page_bytes + ((p_tile * TILE & (c.ps - 1)) >> 4) * GROUP, STAGE, bar);
       }
     }
     --left;
+    if (++p_tile == sq.tiles) {  // on to the next item, if there is one in the run
+      p_tile = win_end = 0;
+      if (++pr == sq.rb) {
+        pr = 0;
+        if (++ph == c.Hkv && left > 0) {
+          ph = 0;
+          do sq = seq_of<ROWS, TILE>(a, ++pi);
+          while (sq.tiles == 0);
+        }
+      }
+    }
   };
 #pragma unroll 1
   for (int s = 0; s < STAGES && left > 0; ++s) request(s);
 
   // ---- the arithmetic's side
-  int ci = i0, item, tile;
-  Seq cs = seq_of<ROWS>(a, i0);
-  item = (int)(off / cs.tiles);
-  tile = (int)(off % cs.tiles);
-  long long todo = t1 - t0;
-  int stage = 0;
+  Seq cs = first;
+  int ci = i0, item = item0, tile = tile0, todo = (int)(t1 - t0), stage = 0;
   uint32_t parity = 0;
   bool fine = true;
   while (todo > 0 && fine) {
     // one segment: tiles [tile, end) of item
-    const int end = (int)min((long long)cs.tiles, tile + todo);
+    const int end = min(cs.tiles, tile + todo);
     const int h = item / cs.rb, row0 = (item % cs.rb) * ROWS, rows = min(ROWS, cs.nq * a.G - row0);
     const long long base = t1 - todo - tile;  // first tile of the item in the line
     uint32_t qf[NT][KSTEPS][2];
@@ -305,8 +177,8 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
         }
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        ex = max(-114, min(100, 13 - ((int)(__float_as_uint(amax) >> 23) - 127)));  // largest value to [2^13, 2^14)
-        const float by = __uint_as_float((uint32_t)(127 + ex) << 23);
+        ex = row_exponent(amax);
+        const float by = exp2i(ex);
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) {
           const float2 x = two_of(src, raw[k]);
@@ -322,7 +194,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
       for (int k = 0; k < 2; ++k) {  // columns 2 cq + k of the scores
         const int col = 8 * nt + 2 * cq + k;
         const int e = __shfl_sync(0xffffffffu, ex, (2 * cq + k) * 4);
-        f[nt][k] = up * __uint_as_float((uint32_t)(127 - e) << 23);
+        f[nt][k] = up * exp2i(-e);
         mref[nt][k] = NO_MAX;
         l[nt][k] = 0.f;
         const int j = (row0 + col) / a.G;
@@ -355,10 +227,6 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint8_t* gp = st + u * GROUP;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sc[u][nt][k] = 0.f;
 #pragma unroll
         for (int half = 0; half < (D == 256 ? 2 : 1); ++half) {
           constexpr int W = D == 64 ? 2 : 4;  // words of a lane: 8 channels each
@@ -394,8 +262,11 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-                mma_f16(sc[u][nt], x[2 * k], y[2 * k], x[2 * k + 1], y[2 * k + 1], qf[nt][half * 8 + 2 * w + k][0], qf[nt][half * 8 + 2 * w + k][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                const int step = half * 8 + 2 * w + k;
+                if (step == 0) mma_f16_first(sc[u][nt], x[0], y[0], x[1], y[1], qf[nt][0][0], qf[nt][0][1]);
+                else mma_f16(sc[u][nt], x[2 * k], y[2 * k], x[2 * k + 1], y[2 * k + 1], qf[nt][step][0], qf[nt][step][1]);
+              }
           }
         }
       }
@@ -412,14 +283,17 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
           }
       }
       // softmax in base 2, relative to mref (7 below the reference maximum)
-      bool raise = false;
+      float x[2][NT][4], top = NEG_INF;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) raise |= fmaf(sc[u][nt][k], f[nt][k & 1], -mref[nt][k & 1]) > 15.0f;
-      if (__any_sync(0xffffffffu, raise)) {
+          for (int k = 0; k < 4; ++k) {
+            x[u][nt][k] = fmaf(sc[u][nt][k], f[nt][k & 1], -mref[nt][k & 1]);
+            top = fmaxf(top, x[u][nt][k]);
+          }
+      if (__any_sync(0xffffffffu, top > 15.0f)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -436,6 +310,8 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
               o[mt][nt][k] *= corr;
               o[mt][nt][k + 2] *= corr;
             }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[v >> 1][nt][k + 2 * (v & 1)] = fmaf(sc[v >> 1][nt][k + 2 * (v & 1)], f[nt][k], -next);
           }
       }
       uint32_t pb[2][NT][2], pl[2][NT][2];
@@ -445,7 +321,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
         for (int nt = 0; nt < NT; ++nt) {
           float p[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) p[k] = ex2(fmaf(sc[u][nt][k], f[nt][k & 1], -mref[nt][k & 1]));
+          for (int k = 0; k < 4; ++k) p[k] = ex2(x[u][nt][k]);
           l[nt][0] += p[0] + p[2];
           l[nt][1] += p[1] + p[3];
 #pragma unroll
@@ -464,19 +340,19 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
         // the lane's entries: MMA columns 2 cq, 2 cq + 1, and 8 further
         const int ta = 2 * cq + (cq & 1), tb = 2 * cq + 1 - (cq & 1);
         constexpr int VW = D / 64;  // words of 8 channels per entry and lane: channels 8 VW g ..
-        uint32_t x[4][VW];
+        uint32_t code[4][VW];
         uint32_t s[2][D == 256 ? 2 : 1];  // scales of (ta, tb) and (ta + 8, tb + 8), per block of the lane
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint8_t* p = gp + ((k & 1 ? tb : ta) + 8 * (k >> 1)) * (D / 2) + g * 4 * VW;
-          if constexpr (VW == 1) x[k][0] = *reinterpret_cast<const uint32_t*>(p);
+          if constexpr (VW == 1) code[k][0] = *reinterpret_cast<const uint32_t*>(p);
           if constexpr (VW == 2) {
             const uint2 v = *reinterpret_cast<const uint2*>(p);
-            x[k][0] = v.x, x[k][1] = v.y;
+            code[k][0] = v.x, code[k][1] = v.y;
           }
           if constexpr (VW == 4) {
             const uint4 v = *reinterpret_cast<const uint4*>(p);
-            x[k][0] = v.x, x[k][1] = v.y, x[k][2] = v.z, x[k][3] = v.w;
+            code[k][0] = v.x, code[k][1] = v.y, code[k][2] = v.z, code[k][3] = v.w;
           }
         }
 #pragma unroll
@@ -503,7 +379,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
           uint32_t lo[2][4], hi[2][4];  // even and odd channels of the word, entries (ta, tb) / (ta + 8, tb + 8)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const uint32_t p = x[2 * k][w], r = x[2 * k + 1][w];
+            const uint32_t p = code[2 * k][w], r = code[2 * k + 1][w];
             kv4_f16_e2m1((p & 0x0f0f0f0fu) | ((r << 4) & 0xf0f0f0f0u), lo[k]);
             kv4_f16_e2m1(((p >> 4) & 0x0f0f0f0fu) | (r & 0xf0f0f0f0u), hi[k]);
             const uint32_t by = s[k][D == 256 ? w / 2 : 0];
@@ -555,13 +431,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
               v[2 * b] = o[m + b][nt][k] * inv;
               v[2 * b + 1] = o[m + b][nt][k + 2] * inv;
             }
-            if constexpr (sizeof(OutT) == 2) {
-              *reinterpret_cast<uint4*>(dst + 2 * m) =
-                  make_uint4(pack_two(dst, v[0], v[1]), pack_two(dst, v[2], v[3]), pack_two(dst, v[4], v[5]), pack_two(dst, v[6], v[7]));
-            } else {
-              *reinterpret_cast<float4*>(dst + 2 * m) = make_float4(v[0], v[1], v[2], v[3]);
-              *reinterpret_cast<float4*>(dst + 2 * m + 4) = make_float4(v[4], v[5], v[6], v[7]);
-            }
+            put8(dst + 2 * m, v);
           }
           if (lse && g == 0) lse[at] = l[nt][k] == 0.f ? NEG_INF : (mref[nt][k] + log2f(l[nt][k])) * LN2;
         } else {
@@ -577,7 +447,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
       tile = 0;
       if (++item == cs.rb * c.Hkv) {
         item = 0;
-        do cs = seq_of<ROWS>(a, ++ci);
+        do cs = seq_of<ROWS, TILE>(a, ++ci);
         while (cs.tiles == 0);
       }
     }
@@ -589,124 +459,15 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
   }
 }
 
-// Joins the partial results of the items that several warps share, and writes the rows that see nothing.  Block = (query token,
-// query head); its warps take the partial results in turn, so that all of them are asked for at once.
-template <int D, int NT, typename OutT>
-__global__ void __launch_bounds__(MERGE_THREADS) k_kv4_merge(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
-  constexpr int ROWS = 8 * NT, CH = D / 32, WARPS = MERGE_THREADS / 32;
-  __shared__ float s_acc[WARPS][D], s_m[WARPS], s_l[WARPS];
-  const int t = blockIdx.x, head = blockIdx.y, h = head / a.G, j = head % a.G, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int i = kv4_find(a.cu, a.c.n_seqs, t);
-  if (i < 0) return;
-  const Seq s = seq_of<ROWS>(a, i);
-  const float vup = kv4_pow2(kv4_exp(a.c.v_exp, h));
-  const int r = (t - s.first) * a.G + j;
-  float acc[CH], total = 0.f, m = NO_MAX;
-#pragma unroll
-  for (int k = 0; k < CH; ++k) acc[k] = 0.f;
-  pdl_wait();
-  if (s.tiles) {
-    const Deal deal = *a.ws.deal;
-    const long long base = a.ws.cum[i] + ((long long)h * s.rb + r / ROWS) * s.tiles;
-    auto worker_of = [&](long long x) {
-      const long long big = deal.rest * (deal.q + 1);
-      if (((big | x) >> 31) == 0) {
-        const unsigned q = (unsigned)deal.q;
-        return x < big ? (int)((unsigned)x / (q + 1)) : (int)deal.rest + (int)((unsigned)(x - big) / q);
-      }
-      return (int)(x < big ? x / (deal.q + 1) : deal.rest + (x - big) / deal.q);
-    };
-    const int w0 = worker_of(base), w1 = worker_of(base + s.tiles - 1);
-    if (w0 == w1) return;  // written where it was computed
-    // worker w's result: its run began ahead of the item, but for the first one's
-    const float* part = a.ws.part + (size_t)(r % ROWS) * (D + 4);
-    for (int b = w0 + warp * 32; b <= w1; b += MERGE_THREADS) {
-      const int mine = b + lane;
-      float2 ml = make_float2(NO_MAX, 0.f);
-      if (mine <= w1) ml = *reinterpret_cast<const float2*>(part + (size_t)(2 * mine + (mine == w0 ? 1 : 0)) * (ROWS * (D + 4)) + D);
-      float mb = ml.x;
-#pragma unroll
-      for (int x = 1; x < 32; x <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, x));
-      mb = fmaxf(mb, m);
-      const float corr = ex2(m - mb), e = ex2(ml.x - mb);
-      m = mb;
-      float le = ml.y * e;
-#pragma unroll
-      for (int x = 1; x < 32; x <<= 1) le += __shfl_xor_sync(0xffffffffu, le, x);
-      total = fmaf(total, corr, le);
-#pragma unroll
-      for (int k = 0; k < CH; ++k) acc[k] *= corr;
-      const int n = min(32, w1 + 1 - b);
-#pragma unroll 8
-      for (int x = 0; x < n; ++x) {
-        const int w = b + x;
-        const float by = __shfl_sync(0xffffffffu, e, x);
-        const float* p = part + (size_t)(2 * w + (w == w0 ? 1 : 0)) * (ROWS * (D + 4));
-        if constexpr (CH == 2) {
-          const float2 v = *reinterpret_cast<const float2*>(p + 2 * lane);
-          acc[0] = fmaf(v.x, by, acc[0]), acc[1] = fmaf(v.y, by, acc[1]);
-        } else {
-#pragma unroll
-          for (int k = 0; k < CH; k += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(p + CH * lane + k);
-            acc[k] = fmaf(v.x, by, acc[k]), acc[k + 1] = fmaf(v.y, by, acc[k + 1]);
-            acc[k + 2] = fmaf(v.z, by, acc[k + 2]), acc[k + 3] = fmaf(v.w, by, acc[k + 3]);
-          }
-        }
-      }
-    }
-    if (w1 - w0 >= 32) {  // (the same for the whole block)
-#pragma unroll
-      for (int k = 0; k < CH; ++k) s_acc[warp][CH * lane + k] = acc[k];
-      if (lane == 0) s_m[warp] = m, s_l[warp] = total;
-      __syncthreads();
-      if (warp) return;
-#pragma unroll
-      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_m[w]);
-      total = 0.f;
-#pragma unroll
-      for (int k = 0; k < CH; ++k) acc[k] = 0.f;
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const float by = ex2(s_m[w] - m);
-        total = fmaf(s_l[w], by, total);
-#pragma unroll
-        for (int k = 0; k < CH; ++k) acc[k] = fmaf(s_acc[w][CH * lane + k], by, acc[k]);
-      }
-    }
-  }
-  if (warp) return;
-  const size_t at = (size_t)t * a.H + head;
-  const float inv = total == 0.f ? 0.f : vup / total;
-  OutT* dst = out + at * D + CH * lane;
-#pragma unroll
-  for (int k = 0; k < CH; k += 2) {
-    if constexpr (sizeof(OutT) == 2) *reinterpret_cast<uint32_t*>(dst + k) = pack_two(dst, acc[k] * inv, acc[k + 1] * inv);
-    else *reinterpret_cast<float2*>(dst + k) = make_float2(acc[k] * inv, acc[k + 1] * inv);
-  }
-  if (lse && lane == 0) lse[at] = total == 0.f ? NEG_INF : (m + log2f(total)) * LN2;
-}
-
-int sm_count() {
-  static int counts[64] = {};  // (threads that look it up at the same time store the same value)
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (!counts[dev]) {
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    counts[dev] = n;
-  }
-  return counts[dev];
-}
-constexpr int MOST_SMS = 160;  // workspaces are sized for this many; the grid never has more CTAs
-
-size_t workspace(const Kv4& c, int rows, int d, int nt, uint8_t* base, AttnWs* ws) {
+// ------------------------------------------------------------------ host side
+size_t workspace(const Kv4& c, long long rows, int nt, uint8_t* base, AttnWs* ws) {
   const size_t cum = 256, part = cum + kv4_align(8 * (size_t)c.n_seqs);
   if (ws) *ws = {(Deal*)base, (long long*)(base + cum), (float*)(base + part)};
   // no more workers than tiles
-  const double tiles = (double)c.n_seqs * ((double)c.max_pages * c.ps / TILE + 1) * c.Hkv * ((rows + 8 * nt - 1) / (8 * nt));
-  const size_t workers = (size_t)(tiles < MOST_SMS * warps_of(d, nt) ? tiles : MOST_SMS * warps_of(d, nt));
-  return part + kv4_align(2 * workers * 8 * nt * (d + 4) * 4);
+  const double tiles = (double)c.n_seqs * ((double)c.max_pages * c.ps / TILE + 1) * c.Hkv * (double)((rows + 8 * nt - 1) / (8 * nt));
+  const int most = MOST_SMS * warps_of(c.d, nt);
+  const size_t workers = tiles < most ? (size_t)tiles : (size_t)most;
+  return part + kv4_align(2 * workers * 8 * nt * (c.d + 4) * 4);
 }
 
 template <int D, int NT, bool TWO, typename T, typename OutT>
@@ -721,7 +482,8 @@ cudaError_t launch(const AttnArgs& a, const void* q, void* out, float* lse, int 
     *done = true;
   }
   cudaError_t e = kv4_launch(k_kv4_stream<D, NT, TWO, T, OutT>, dim3(grid), warps_of(D, NT) * 32, smem, s, false, a, (const T*)q, (OutT*)out, lse);
-  if (e == cudaSuccess) e = kv4_launch(k_kv4_merge<D, NT, OutT>, dim3(a.n_tokens, a.H), MERGE_THREADS, 0, s, true, a, (OutT*)out, lse);
+  if (e == cudaSuccess)
+    e = kv4_launch(k_kv4_merge<D, 8 * NT, TILE, OutT>, dim3(a.n_tokens, a.H), MERGE_THREADS, 0, s, true, a, (OutT*)out, lse);
   return e;
 }
 
@@ -732,14 +494,26 @@ cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* 
   return out_f32 ? launch<D, NT, true, __half, float>(a, q, out, lse, grid, s) : launch<D, NT, true, __half, __half>(a, q, out, lse, grid, s);
 }
 
+// query rows of a KV head in the longest sequence
+long long rows_of(const Kv4& c, bool ragged, int max_q, int n_q_heads) { return (long long)(ragged ? (max_q > 0 ? max_q : 1) : 1) * (n_q_heads / c.Hkv); }
+
 }  // namespace
 
-size_t kv4_attention_workspace(const Kv4& c, int n_tokens, int n_q_heads) {
-  // (rows: what the longest sequence could bring; both row-block sizes are covered)
-  const long long rows = (long long)n_tokens * (n_q_heads / c.Hkv);
-  const int r = (int)(rows < (1 << 20) ? rows : 1 << 20);
-  const size_t x = workspace(c, r, c.d, 1, nullptr, nullptr), y = workspace(c, r, c.d, 2, nullptr, nullptr);
-  return x > y ? x : y;
+int kv4_sm_count() {
+  static int counts[64] = {};  // (threads that look it up at the same time store the same value)
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  if (!counts[dev]) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    counts[dev] = n < MOST_SMS ? n : MOST_SMS;
+  }
+  return counts[dev];
+}
+
+size_t kv4_attention_workspace(const Kv4& c, int max_q, int n_q_heads) {
+  const long long rows = rows_of(c, true, max_q, n_q_heads);
+  return workspace(c, rows, rows <= 8 ? 1 : 2, nullptr, nullptr);
 }
 
 extern "C" int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int dtype, const void* q, long long q_stride, int n_tokens,
@@ -759,17 +533,16 @@ extern "C" int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int 
   if (q_stride < dense || q_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3))
     return kv4_fail(IM_ERR_ARG, fn, "the token stride must be a multiple of 8 elements, no shorter than a token; bases 16-byte aligned");
   if (!(softmax_scale >= 0.f) || isinf(softmax_scale)) return kv4_fail(IM_ERR_ARG, fn, "softmax_scale must be positive (0: 1/sqrt(head_dim))");
-  if (!workspace_ || ((uintptr_t)workspace_ & 255) || workspace_bytes < kv4_attention_workspace(c, n_tokens, n_q_heads))
+  if (!workspace_ || ((uintptr_t)workspace_ & 255) || workspace_bytes < kv4_attention_workspace(c, cu_q ? max_q : 1, n_q_heads))
     return kv4_fail(IM_ERR_CAPACITY, fn, "workspace missing, misaligned or too small");
   if (!n_tokens) return IM_OK;
-  const int sms = sm_count();
-  if (sms < 1) return kv4_fail(IM_ERR_CUDA, fn, "no usable CUDA device");
+  const int grid = kv4_sm_count();
+  if (grid < 1) return kv4_fail(IM_ERR_CUDA, fn, "no usable CUDA device");
   AttnArgs a = {c, map->table, map->lens, cu_q, q_stride, n_tokens, n_q_heads, n_q_heads / c.Hkv, causal ? 1 : 0,
                 softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)c.d), {}};
-  const long long rows = (long long)(cu_q ? max_q : 1) * a.G;
+  const long long rows = rows_of(c, cu_q != nullptr, max_q, n_q_heads);
   const int nt = rows <= 8 ? 1 : 2;
-  workspace(c, 1, c.d, nt, (uint8_t*)workspace_, &a.ws);
-  const int grid = sms < MOST_SMS ? sms : MOST_SMS;
+  workspace(c, rows, nt, (uint8_t*)workspace_, &a.ws);
   cudaStream_t s = (cudaStream_t)cuda_stream;
   auto go = [&](auto dim) {
     constexpr int D = decltype(dim)::value;

@@ -1,0 +1,264 @@
+// Shared by the kernels of im_kv4_attention (im_kv4_attn.cu: few query rows; im_kv4_chunk.cu: many): how a call's work is dealt to
+// workers of equal share, and how their partial results are joined.
+//
+// The entries of all items (sequence, KV head, row block) form one line of tiles, sequence-major; a worker gets an equal run
+// of it whatever the lengths are, which the device alone knows.  An item that one worker runs through is written by it; of
+// the others the workers leave (sum of p v, reference maximum, sum of p) in the workspace, and k_kv4_merge adds those up in
+// order of the workers: results do not depend on timing.
+#pragma once
+#include <type_traits>
+
+#include "im_kv4.cuh"
+
+namespace {
+
+constexpr float NEG_INF = -__builtin_huge_valf();
+constexpr float NO_MAX = -1e30f;  // reference maximum of a row that has seen nothing
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int MERGE_THREADS = 128;
+constexpr int MOST_SMS = 160;     // workspaces are sized for this many; a grid never has more CTAs
+
+struct Deal {
+  long long q, rest;  // the first `rest` workers get q + 1 tiles, the others q
+};
+struct AttnWs {
+  Deal* deal;
+  long long* cum;  // [n_seqs] tiles ahead of the sequence
+  float* part;     // [2 * workers][ROWS][D + 4]
+};
+struct AttnArgs {
+  Kv4 c;
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* cu;
+  long long q_stride;
+  int n_tokens, H, G, causal;
+  float scale;
+  AttnWs ws;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float2 two_of(const bf16*, uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t pack_two(const bf16*, float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_two(const __half*, float a, float b) { return pack_f16(a, b); }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+// eight values of a row to `dst`, in its type
+template <typename OutT>
+__device__ __forceinline__ void put8(OutT* dst, const float* v) {
+  if constexpr (sizeof(OutT) == 2) {
+    *reinterpret_cast<uint4*>(dst) = make_uint4(pack_two(dst, v[0], v[1]), pack_two(dst, v[2], v[3]), pack_two(dst, v[4], v[5]), pack_two(dst, v[6], v[7]));
+  } else {
+    reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+// power of two that brings a row's largest bf16 value to [2^13, 2^14): the row then fits f16, values down to 2^-29 of the
+// largest exactly
+__device__ __forceinline__ int row_exponent(float amax) { return max(-114, min(100, 13 - ((int)(__float_as_uint(amax) >> 23) - 127))); }
+__device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// query tokens of sequence i, clipped to the tensors
+__device__ __forceinline__ void queries_of(const AttnArgs& a, int i, int* first, int* count) {
+  if (!a.cu) {
+    *first = i;
+    *count = 1;
+    return;
+  }
+  const int s = max(0, min(a.n_tokens, a.cu[i])), e = max(s, min(a.n_tokens, a.cu[i + 1]));
+  *first = s;
+  *count = e - s;
+}
+
+struct Seq {
+  int L, first, nq, tiles, rb;  // rb: row blocks
+};
+template <int ROWS, int TILE>
+__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int i) {
+  Seq s;
+  s.L = (int)max(0ll, min((long long)a.lens[i], (long long)a.c.max_pages * a.c.ps));
+  queries_of(a, i, &s.first, &s.nq);
+  s.rb = (int)(((long long)s.nq * a.G + ROWS - 1) / ROWS);
+  s.tiles = s.nq ? (s.L + TILE - 1) / TILE : 0;
+  return s;
+}
+__device__ __forceinline__ long long work_of(const AttnArgs& a, const Seq& s) { return (long long)s.tiles * s.rb * a.c.Hkv; }
+
+// Adds the sequences up (every CTA for itself) and deals the line to at most `most` workers.  s_cum [THREADS + 1]: tiles
+// ahead of each thread's run of `per` sequences.  Ends with a block barrier.
+template <int ROWS, int TILE, int THREADS>
+__device__ __forceinline__ Deal deal_line(const AttnArgs& a, long long* s_cum, long long* s_scan, long long most, int* workers, int* per_) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = a.c.n_seqs;
+  const int per = (n + THREADS - 1) / THREADS;
+  long long mine = 0;
+  for (int i = tid * per; i < min(n, tid * per + per); ++i) mine += work_of(a, seq_of<ROWS, TILE>(a, i));
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31) s_scan[warp] = incl;
+  __syncthreads();
+  long long before = 0;
+  for (int w = 0; w < warp; ++w) before += s_scan[w];
+  s_cum[tid] = before + incl - mine;
+  if (tid == THREADS - 1) s_cum[THREADS] = before + incl;
+  __syncthreads();
+  const long long total = s_cum[THREADS];
+  *workers = (int)min(most, max(1ll, total));
+  *per_ = per;
+  const Deal d = {total / *workers, total % *workers};
+  if (blockIdx.x == 0) {
+    if (tid == 0) *a.ws.deal = d;
+    long long at = s_cum[tid];
+    for (int i = tid * per; i < min(n, tid * per + per); ++i) {
+      a.ws.cum[i] = at;
+      at += work_of(a, seq_of<ROWS, TILE>(a, i));
+    }
+  }
+  return d;
+}
+// the sequence that tile t (< total) of the line lies in, and the tile's place in it
+template <int ROWS, int TILE, int THREADS>
+__device__ __forceinline__ int find_tile(const AttnArgs& a, const long long* s_cum, int per, long long t, long long* off) {
+  int lo = 0, hi = THREADS;  // s_cum[lo] <= t < s_cum[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (s_cum[mid] <= t) lo = mid;
+    else hi = mid;
+  }
+  int i = lo * per;
+  *off = t - s_cum[lo];
+  while (true) {
+    const long long w = work_of(a, seq_of<ROWS, TILE>(a, i));
+    if (*off < w) return i;
+    *off -= w;
+    ++i;
+  }
+}
+
+// Joins the partial results of the items that several warps share, and writes the rows that see nothing.  Block = (query token,
+// query head); its warps take the partial results in turn, so that all of them are asked for at once.
+template <int D, int ROWS, int TILE, typename OutT>
+__global__ void __launch_bounds__(MERGE_THREADS) k_kv4_merge(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
+  constexpr int CH = D / 32, WARPS = MERGE_THREADS / 32;
+  __shared__ float s_acc[WARPS][D], s_m[WARPS], s_l[WARPS];
+  const int t = blockIdx.x, head = blockIdx.y, h = head / a.G, j = head % a.G, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int i = kv4_find(a.cu, a.c.n_seqs, t);
+  if (i < 0) return;
+  const Seq s = seq_of<ROWS, TILE>(a, i);
+  const float vup = kv4_pow2(kv4_exp(a.c.v_exp, h));
+  const int r = (t - s.first) * a.G + j;
+  float acc[CH], total = 0.f, m = NO_MAX;
+#pragma unroll
+  for (int k = 0; k < CH; ++k) acc[k] = 0.f;
+  pdl_wait();
+  if (s.tiles) {
+    const Deal deal = *a.ws.deal;
+    const long long base = a.ws.cum[i] + ((long long)h * s.rb + r / ROWS) * s.tiles;
+    auto worker_of = [&](long long x) {
+      const long long big = deal.rest * (deal.q + 1);
+      if (((big | x) >> 31) == 0) {
+        const unsigned q = (unsigned)deal.q;
+        return x < big ? (int)((unsigned)x / (q + 1)) : (int)deal.rest + (int)((unsigned)(x - big) / q);
+      }
+      return (int)(x < big ? x / (deal.q + 1) : deal.rest + (x - big) / deal.q);
+    };
+    const int w0 = worker_of(base), w1 = worker_of(base + s.tiles - 1);
+    if (w0 == w1) return;  // written where it was computed
+    // worker w's result: its run began ahead of the item, but for the first one's
+    const float* part = a.ws.part + (size_t)(r % ROWS) * (D + 4);
+    for (int b = w0 + warp * 32; b <= w1; b += MERGE_THREADS) {
+      const int mine = b + lane;
+      float2 ml = make_float2(NO_MAX, 0.f);
+      if (mine <= w1) ml = *reinterpret_cast<const float2*>(part + (size_t)(2 * mine + (mine == w0 ? 1 : 0)) * (ROWS * (D + 4)) + D);
+      float mb = ml.x;
+#pragma unroll
+      for (int x = 1; x < 32; x <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, x));
+      mb = fmaxf(mb, m);
+      const float corr = ex2(m - mb), e = ex2(ml.x - mb);
+      m = mb;
+      float le = ml.y * e;
+#pragma unroll
+      for (int x = 1; x < 32; x <<= 1) le += __shfl_xor_sync(0xffffffffu, le, x);
+      total = fmaf(total, corr, le);
+#pragma unroll
+      for (int k = 0; k < CH; ++k) acc[k] *= corr;
+      const int n = min(32, w1 + 1 - b);
+#pragma unroll 8
+      for (int x = 0; x < n; ++x) {
+        const int w = b + x;
+        const float by = __shfl_sync(0xffffffffu, e, x);
+        const float* p = part + (size_t)(2 * w + (w == w0 ? 1 : 0)) * (ROWS * (D + 4));
+        if constexpr (CH == 2) {
+          const float2 v = *reinterpret_cast<const float2*>(p + 2 * lane);
+          acc[0] = fmaf(v.x, by, acc[0]), acc[1] = fmaf(v.y, by, acc[1]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < CH; k += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p + CH * lane + k);
+            acc[k] = fmaf(v.x, by, acc[k]), acc[k + 1] = fmaf(v.y, by, acc[k + 1]);
+            acc[k + 2] = fmaf(v.z, by, acc[k + 2]), acc[k + 3] = fmaf(v.w, by, acc[k + 3]);
+          }
+        }
+      }
+    }
+    if (w1 - w0 >= 32) {  // (the same for the whole block)
+#pragma unroll
+      for (int k = 0; k < CH; ++k) s_acc[warp][CH * lane + k] = acc[k];
+      if (lane == 0) s_m[warp] = m, s_l[warp] = total;
+      __syncthreads();
+      if (warp) return;
+#pragma unroll
+      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_m[w]);
+      total = 0.f;
+#pragma unroll
+      for (int k = 0; k < CH; ++k) acc[k] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float by = ex2(s_m[w] - m);
+        total = fmaf(s_l[w], by, total);
+#pragma unroll
+        for (int k = 0; k < CH; ++k) acc[k] = fmaf(s_acc[w][CH * lane + k], by, acc[k]);
+      }
+    }
+  }
+  if (warp) return;
+  const size_t at = (size_t)t * a.H + head;
+  const float inv = total == 0.f ? 0.f : vup / total;
+  OutT* dst = out + at * D + CH * lane;
+#pragma unroll
+  for (int k = 0; k < CH; k += 2) {
+    if constexpr (sizeof(OutT) == 2) *reinterpret_cast<uint32_t*>(dst + k) = pack_two(dst, acc[k] * inv, acc[k + 1] * inv);
+    else *reinterpret_cast<float2*>(dst + k) = make_float2(acc[k] * inv, acc[k + 1] * inv);
+  }
+  if (lse && lane == 0) lse[at] = total == 0.f ? NEG_INF : (m + log2f(total)) * LN2;
+}
+
+}  // namespace
+
+// number of SMs of the current device (0: none)
+int kv4_sm_count();
