@@ -732,10 +732,10 @@ class KV4Cache:
         qs = self._rows_of(q, H, "q")
         dtype = torch.float32 if out_f32 else q.dtype
         if out is None:
-            out = q.new_empty((n, H, self.head_dim)) if not out_f32 else torch.empty((n, H, self.head_dim), dtype=dtype, device=self.device)
+            out = torch.empty_like(q) if dtype == q.dtype and q.is_contiguous() else q.new_empty((n, H, self.head_dim), dtype=dtype)
         elif out.device != self.device or out.dtype != dtype or tuple(out.shape) != (n, H, self.head_dim) or not out.is_contiguous():
             raise ValueError(f"out: need a contiguous {dtype} tensor {(n, H, self.head_dim)} on {self.device}")
-        lse = torch.empty((n, H), dtype=torch.float32, device=self.device) if return_lse else None
+        lse = q.new_empty((n, H), dtype=torch.float32) if return_lse else None
         m = self.map if map is None else self._check_map(map)
         ws, nbytes = self._workspace(1, 1 if cu_q is None else max_q, H)
         self._call(_lib.im_kv4_attention, self._p, m._p, _DTYPE_IDS[q.dtype], q.data_ptr(), qs, n, self._starts(cu_q, n, "attend"),

@@ -27,9 +27,10 @@ constexpr int RING_BYTES = 221184;  // shared memory of a CTA's rings
 constexpr int warps_of(int d, int nt) { return d == 256 ? (nt == 1 ? 12 : 8) : nt == 1 ? 16 : 12; }
 constexpr int stages_of(int d, int nt) { return RING_BYTES / (warps_of(d, nt) * 2 * kv4_group_bytes(d)); }
 
+// bounded; the whole warp waits, and gets one answer
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t it = 0; it < IM_WAIT_LIMIT; ++it) {
-    uint32_t done;
+  uint32_t done = 0;
+  for (uint32_t it = 0; it < IM_WAIT_LIMIT && !done; ++it)
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
@@ -37,9 +38,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
         : "=r"(done)
         : "r"(bar), "r"(parity)
         : "memory");
-    if (done) return true;
-  }
-  return false;
+  return __all_sync(0xffffffffu, done);
 }
 __device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -153,7 +152,6 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
     float f[NT][2], mref[NT][2], l[NT][2];
     int lim[NT][2];
     int lim_min = cs.L;
-    const float up = a.scale * LOG2E * kv4_pow2(kv4_exp(c.k_exp, h));
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       // row 8 nt + g: channels in the order the keys' lanes take them
@@ -194,7 +192,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
       for (int k = 0; k < 2; ++k) {  // columns 2 cq + k of the scores
         const int col = 8 * nt + 2 * cq + k;
         const int e = __shfl_sync(0xffffffffu, ex, (2 * cq + k) * 4);
-        f[nt][k] = up * exp2i(-e);
+        f[nt][k] = row_factor(a, h, e);
         mref[nt][k] = NO_MAX;
         l[nt][k] = 0.f;
         const int j = (row0 + col) / a.G;
@@ -496,6 +494,8 @@ cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* 
 
 // query rows of a KV head in the longest sequence
 long long rows_of(const Kv4& c, bool ragged, int max_q, int n_q_heads) { return (long long)(ragged ? (max_q > 0 ? max_q : 1) : 1) * (n_q_heads / c.Hkv); }
+// Which kernel.  Beyond 16 rows (two column tiles) the streaming kernel would unpack the cache again for every 16.
+bool by_chunks(const Kv4& c, long long rows) { return rows > 16 && c.d != 256; }
 
 }  // namespace
 
@@ -513,7 +513,7 @@ int kv4_sm_count() {
 
 size_t kv4_attention_workspace(const Kv4& c, int max_q, int n_q_heads) {
   const long long rows = rows_of(c, true, max_q, n_q_heads);
-  return workspace(c, rows, rows <= 8 ? 1 : 2, nullptr, nullptr);
+  return by_chunks(c, rows) ? kv4_chunk_workspace(c, nullptr, nullptr) : workspace(c, rows, rows <= 8 ? 1 : 2, nullptr, nullptr);
 }
 
 extern "C" int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int dtype, const void* q, long long q_stride, int n_tokens,
@@ -541,9 +541,14 @@ extern "C" int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int 
   AttnArgs a = {c, map->table, map->lens, cu_q, q_stride, n_tokens, n_q_heads, n_q_heads / c.Hkv, causal ? 1 : 0,
                 softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)c.d), {}};
   const long long rows = rows_of(c, cu_q != nullptr, max_q, n_q_heads);
+  cudaStream_t s = (cudaStream_t)cuda_stream;
+  if (by_chunks(c, rows)) {
+    kv4_chunk_workspace(c, (uint8_t*)workspace_, &a.ws);
+    const cudaError_t e = kv4_launch_chunk(a, dtype, out_f32, q, out, lse, grid, s);
+    return e == cudaSuccess ? IM_OK : im_fail_message(IM_ERR_CUDA, cudaGetErrorString(e));
+  }
   const int nt = rows <= 8 ? 1 : 2;
   workspace(c, rows, nt, (uint8_t*)workspace_, &a.ws);
-  cudaStream_t s = (cudaStream_t)cuda_stream;
   auto go = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     return nt == 1 ? launch_types<D, 1>(a, dtype, out_f32, q, out, lse, grid, s) : launch_types<D, 2>(a, dtype, out_f32, q, out, lse, grid, s);

@@ -10,14 +10,6 @@
 
 #include "im_kv4.cuh"
 
-namespace {
-
-constexpr float NEG_INF = -__builtin_huge_valf();
-constexpr float NO_MAX = -1e30f;  // reference maximum of a row that has seen nothing
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int MERGE_THREADS = 128;
-constexpr int MOST_SMS = 160;     // workspaces are sized for this many; a grid never has more CTAs
-
 struct Deal {
   long long q, rest;  // the first `rest` workers get q + 1 tiles, the others q
 };
@@ -36,6 +28,20 @@ struct AttnArgs {
   float scale;
   AttnWs ws;
 };
+
+// number of SMs of the current device (0: none)
+int kv4_sm_count();
+// many query rows (head_dim 64 or 128): workspace (ws, if not null, is set up in `base`), launch
+size_t kv4_chunk_workspace(const Kv4& c, uint8_t* base, AttnWs* ws);
+cudaError_t kv4_launch_chunk(const AttnArgs& a, int dtype, int out_f32, const void* q, void* out, float* lse, int grid, cudaStream_t s);
+
+namespace {
+
+constexpr float NEG_INF = -__builtin_huge_valf();
+constexpr float NO_MAX = -1e30f;  // reference maximum of a row that has seen nothing
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int MERGE_THREADS = 128;
+constexpr int MOST_SMS = 160;     // workspaces are sized for this many; a grid never has more CTAs
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
@@ -79,6 +85,10 @@ __device__ __forceinline__ void put8(OutT* dst, const float* v) {
 // largest exactly
 __device__ __forceinline__ int row_exponent(float amax) { return max(-114, min(100, 13 - ((int)(__float_as_uint(amax) >> 23) - 127))); }
 __device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+// scores times this: base-2 exponents (kept finite and above zero, so that -inf stays -inf)
+__device__ __forceinline__ float row_factor(const AttnArgs& a, int h, int e) {
+  return fmaxf(1e-37f, fminf(1e37f, a.scale * LOG2E * kv4_pow2(kv4_exp(a.c.k_exp, h)) * exp2i(-e)));
+}
 
 // query tokens of sequence i, clipped to the tensors
 __device__ __forceinline__ void queries_of(const AttnArgs& a, int i, int* first, int* count) {
@@ -259,6 +269,3 @@ __global__ void __launch_bounds__(MERGE_THREADS) k_kv4_merge(const AttnArgs a, O
 }
 
 }  // namespace
-
-// number of SMs of the current device (0: none)
-int kv4_sm_count();

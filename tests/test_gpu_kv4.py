@@ -377,24 +377,26 @@ def test_queries_that_are_not_finite_stay_in_their_rows(im):
     assert torch.equal(got[~hurt], clean[~hurt]) and torch.isnan(got[hurt]).all()
 
 
-def test_bad_pages_are_skipped_and_flagged(im):
+@pytest.mark.parametrize("nq", [1, 9])
+def test_bad_pages_are_skipped_and_flagged(im, nq):
     pair = Pair(im, 2, 4, 8, 1, 64, 16, exps=False)
     assert pair.append([50, 20])
-    q = torch.randn(2, 4, 64, device="cuda:0").to(BF)
+    q = torch.randn(2 * nq, 4, 64, device="cuda:0").to(BF)
+    cu = ints([0, nq, 2 * nq])
     m = pair.g.map.clone()
     m.table[0, 1] = 8                                                                    # past the pool
     m.table[1, 0] = -3
-    o, lse = pair.g.attend(q, return_lse=True, out_f32=True, map=m)
+    o, lse = pair.g.attend(q, cu, nq, return_lse=True, out_f32=True, causal=False, map=m)
     assert pair.g.status(clear=True) == im.IM_KV4_BAD_MAP
     r = pair.r
     for i, rows in ((0, list(range(16)) + list(range(32, 50))), (1, list(range(16, 20)))):
         K, V = r.kv(i)
-        s = np.einsum("hd,td->ht", q[i].double().cpu().numpy(), K[rows, 0]) / 8
-        p = np.exp(s - s.max(1, keepdims=True))
-        np.testing.assert_allclose(o[i].double().cpu().numpy(), p @ V[rows, 0] / p.sum(1, keepdims=True), rtol=1e-4, atol=1e-5)
+        s = np.einsum("qhd,td->qht", q[nq * i:nq * i + nq].double().cpu().numpy(), K[rows, 0]) / 8
+        p = np.exp(s - s.max(2, keepdims=True))
+        np.testing.assert_allclose(o[nq * i:nq * i + nq].double().cpu().numpy(), p @ V[rows, 0] / p.sum(2, keepdims=True), rtol=1e-4, atol=1e-5)
     m.lens[0], m.lens[1] = -5, 1000                                                      # lengths out of range: none, and the row's capacity
-    o = pair.g.attend(q, map=m)
-    assert (o[0] == 0).all()
+    o = pair.g.attend(q, cu, nq, map=m)
+    assert (o[:nq] == 0).all()
 
 
 # ------------------------------------------------------------------ together
