@@ -30,6 +30,7 @@ constexpr int stages_of(int d, int nt) { return RING_BYTES / (warps_of(d, nt) * 
 // bounded; the whole warp waits, and gets one answer
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   uint32_t done = 0;
+#pragma unroll 1
   for (uint32_t it = 0; it < IM_WAIT_LIMIT && !done; ++it)
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -218,184 +219,192 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
       const uint8_t* st = ring + stage * STAGE;
       const uint32_t no_page = (bad >> (2 * stage)) & 3u;
       const int e0 = tile * TILE;
-      const bool whole = e0 + TILE <= lim_min && no_page == 0;
-      // entry of MMA row i within a group: i ^ (i >> 1 & 1), so that the lanes of a V load see both halves of the banks
-      const int ra = g ^ ((g >> 1) & 1);
-      float sc[2][NT][4];
+      // (one body for the tiles that every row sees whole, one for the others)
+      auto compute = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        // entry of MMA row i within a group: i ^ (i >> 1 & 1), so that the lanes of a V load see both halves of the banks
+        const int ra = g ^ ((g >> 1) & 1);
+        float sc[2][NT][4];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint8_t* gp = st + u * GROUP;
+        for (int u = 0; u < 2; ++u) {
+          const uint8_t* gp = st + u * GROUP;
 #pragma unroll
-        for (int half = 0; half < (D == 256 ? 2 : 1); ++half) {
-          constexpr int W = D == 64 ? 2 : 4;  // words of a lane: 8 channels each
-          uint32_t ka[W], kb[W], sa, sb;
-          const int at = ra * (D / 2) + half * 64 + cq * 4 * W;
-          if constexpr (W == 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(gp + at), y = *reinterpret_cast<const uint4*>(gp + at + 4 * D);
-            ka[0] = x.x, ka[1] = x.y, ka[2] = x.z, ka[3] = x.w;
-            kb[0] = y.x, kb[1] = y.y, kb[2] = y.z, kb[3] = y.w;
-            sa = *reinterpret_cast<const uint16_t*>(gp + 8 * D + ra * (D / 16) + half * 8 + 2 * cq);
-            sb = *reinterpret_cast<const uint16_t*>(gp + 8 * D + (ra + 8) * (D / 16) + half * 8 + 2 * cq);
-          } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(gp + at), y = *reinterpret_cast<const uint2*>(gp + at + 4 * D);
-            ka[0] = x.x, ka[1] = x.y;
-            kb[0] = y.x, kb[1] = y.y;
-            sa = gp[8 * D + ra * (D / 16) + cq];
-            sb = gp[8 * D + (ra + 8) * (D / 16) + cq];
-          }
-          sa = kv4_f16x2_e4m3(sa);
-          sb = kv4_f16x2_e4m3(sb);
-          const uint32_t fa[2] = {__byte_perm(sa, sa, 0x1010), __byte_perm(sa, sa, 0x3232)};
-          const uint32_t fb[2] = {__byte_perm(sb, sb, 0x1010), __byte_perm(sb, sb, 0x3232)};
-#pragma unroll
-          for (int w = 0; w < W; ++w) {
-            uint32_t x[4], y[4];
-            kv4_f16_e2m1(ka[w], x);
-            kv4_f16_e2m1(kb[w], y);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              x[k] = mul2(x[k], fa[w / 2]);
-              y[k] = mul2(y[k], fb[w / 2]);
+          for (int half = 0; half < (D == 256 ? 2 : 1); ++half) {
+            constexpr int W = D == 64 ? 2 : 4;  // words of a lane: 8 channels each
+            uint32_t ka[W], kb[W], sa, sb;
+            const int at = ra * (D / 2) + half * 64 + cq * 4 * W;
+            if constexpr (W == 4) {
+              const uint4 x = *reinterpret_cast<const uint4*>(gp + at), y = *reinterpret_cast<const uint4*>(gp + at + 4 * D);
+              ka[0] = x.x, ka[1] = x.y, ka[2] = x.z, ka[3] = x.w;
+              kb[0] = y.x, kb[1] = y.y, kb[2] = y.z, kb[3] = y.w;
+              sa = *reinterpret_cast<const uint16_t*>(gp + 8 * D + ra * (D / 16) + half * 8 + 2 * cq);
+              sb = *reinterpret_cast<const uint16_t*>(gp + 8 * D + (ra + 8) * (D / 16) + half * 8 + 2 * cq);
+            } else {
+              const uint2 x = *reinterpret_cast<const uint2*>(gp + at), y = *reinterpret_cast<const uint2*>(gp + at + 4 * D);
+              ka[0] = x.x, ka[1] = x.y;
+              kb[0] = y.x, kb[1] = y.y;
+              sa = gp[8 * D + ra * (D / 16) + cq];
+              sb = gp[8 * D + (ra + 8) * (D / 16) + cq];
             }
+            sa = kv4_f16x2_e4m3(sa);
+            sb = kv4_f16x2_e4m3(sb);
+            const uint32_t fa[2] = {__byte_perm(sa, sa, 0x1010), __byte_perm(sa, sa, 0x3232)};
+            const uint32_t fb[2] = {__byte_perm(sb, sb, 0x1010), __byte_perm(sb, sb, 0x3232)};
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int w = 0; w < W; ++w) {
+              uint32_t x[4], y[4];
+              kv4_f16_e2m1(ka[w], x);
+              kv4_f16_e2m1(kb[w], y);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                const int step = half * 8 + 2 * w + k;
-                if (step == 0) mma_f16_first(sc[u][nt], x[0], y[0], x[1], y[1], qf[nt][0][0], qf[nt][0][1]);
-                else mma_f16(sc[u][nt], x[2 * k], y[2 * k], x[2 * k + 1], y[2 * k + 1], qf[nt][step][0], qf[nt][step][1]);
+              for (int k = 0; k < 4; ++k) {
+                x[k] = mul2(x[k], fa[w / 2]);
+                y[k] = mul2(y[k], fb[w / 2]);
               }
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  const int step = half * 8 + 2 * w + k;
+                  if (step == 0) mma_f16_first(sc[u][nt], x[0], y[0], x[1], y[1], qf[nt][0][0], qf[nt][0][1]);
+                  else mma_f16(sc[u][nt], x[2 * k], y[2 * k], x[2 * k + 1], y[2 * k + 1], qf[nt][step][0], qf[nt][step][1]);
+                }
+            }
           }
         }
-      }
-      if (!whole) {
+        if constexpr (!WHOLE) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int e = e0 + 16 * u + ra + 8 * (k >> 1);
+              const bool gone = (no_page >> u) & 1u;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                if (gone || e >= lim[nt][k & 1]) sc[u][nt][k] = NEG_INF;
+            }
+        }
+        // softmax in base 2, relative to mref (7 below the reference maximum)
+        float x[2][NT][4], top = NEG_INF;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+              const float2 e = fma2(make_float2(sc[u][nt][k], sc[u][nt][k + 1]), make_float2(f[nt][0], f[nt][1]), make_float2(-mref[nt][0], -mref[nt][1]));
+              x[u][nt][k] = e.x;
+              x[u][nt][k + 1] = e.y;
+              top = max3(top, e.x, e.y);
+            }
+        if (__any_sync(0xffffffffu, top > 15.0f)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float m = fmaxf(fmaxf(sc[0][nt][k], sc[0][nt][k + 2]), fmaxf(sc[1][nt][k], sc[1][nt][k + 2])) * f[nt][k];
+#pragma unroll
+              for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+              const float next = m - mref[nt][k] > 15.0f ? m - 7.0f : mref[nt][k];
+              const float corr = ex2(mref[nt][k] - next);
+              mref[nt][k] = next;
+              l[nt][k] *= corr;
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                o[mt][nt][k] *= corr;
+                o[mt][nt][k + 2] *= corr;
+              }
+#pragma unroll
+              for (int v = 0; v < 4; ++v) x[v >> 1][nt][k + 2 * (v & 1)] = fmaf(sc[v >> 1][nt][k + 2 * (v & 1)], f[nt][k], -next);
+            }
+        }
+        uint32_t pb[2][NT][2], pl[2][NT][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float p[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) p[k] = ex2(x[u][nt][k]);
+            const float2 sum = add2(make_float2(l[nt][0], l[nt][1]), add2(make_float2(p[0], p[1]), make_float2(p[2], p[3])));
+            l[nt][0] = sum.x;
+            l[nt][1] = sum.y;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t hi = pack_f16(p[2 * k], p[2 * k + 1]);
+              pb[u][nt][k] = transpose8x8(hi);
+              if constexpr (TWO) {
+                const float2 back = kv4_unpack_f16(hi);
+                pl[u][nt][k] = transpose8x8(pack_f16(p[2 * k] - back.x, p[2 * k + 1] - back.y));
+              }
+            }
+          }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint8_t* gp = st + u * GROUP + 9 * D;
+          // the lane's entries: MMA columns 2 cq, 2 cq + 1, and 8 further
+          const int ta = 2 * cq + (cq & 1), tb = 2 * cq + 1 - (cq & 1);
+          constexpr int VW = D / 64;  // words of 8 channels per entry and lane: channels 8 VW g ..
+          uint32_t code[4][VW];
+          uint32_t s[2][D == 256 ? 2 : 1];  // scales of (ta, tb) and (ta + 8, tb + 8), per block of the lane
+#pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const int e = e0 + 16 * u + ra + 8 * (k >> 1);
-            const bool gone = (no_page >> u) & 1u;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              if (gone || e >= lim[nt][k & 1]) sc[u][nt][k] = NEG_INF;
+            const uint8_t* p = gp + ((k & 1 ? tb : ta) + 8 * (k >> 1)) * (D / 2) + g * 4 * VW;
+            if constexpr (VW == 1) code[k][0] = *reinterpret_cast<const uint32_t*>(p);
+            if constexpr (VW == 2) {
+              const uint2 v = *reinterpret_cast<const uint2*>(p);
+              code[k][0] = v.x, code[k][1] = v.y;
+            }
+            if constexpr (VW == 4) {
+              const uint4 v = *reinterpret_cast<const uint4*>(p);
+              code[k][0] = v.x, code[k][1] = v.y, code[k][2] = v.z, code[k][3] = v.w;
+            }
           }
-      }
-      // softmax in base 2, relative to mref (7 below the reference maximum)
-      float x[2][NT][4], top = NEG_INF;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            x[u][nt][k] = fmaf(sc[u][nt][k], f[nt][k & 1], -mref[nt][k & 1]);
-            top = fmaxf(top, x[u][nt][k]);
-          }
-      if (__any_sync(0xffffffffu, top > 15.0f)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            float m = fmaxf(fmaxf(sc[0][nt][k], sc[0][nt][k + 2]), fmaxf(sc[1][nt][k], sc[1][nt][k + 2])) * f[nt][k];
+            const uint8_t* p = gp + 8 * D + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
+            uint32_t sa, sb;
+            if constexpr (D == 256) {
+              sa = *reinterpret_cast<const uint16_t*>(p + (ta + 8 * k) * (D / 16));
+              sb = *reinterpret_cast<const uint16_t*>(p + (tb + 8 * k) * (D / 16));
+            } else {
+              sa = p[(ta + 8 * k) * (D / 16)];
+              sb = p[(tb + 8 * k) * (D / 16)];
+            }
+            if constexpr (!WHOLE) {  // what lies behind the sequence may be anything, a scale's NaN too
+              const int e = e0 + 16 * u + 8 * k;
+              if (((no_page >> u) & 1u) || e + ta >= cs.L) sa = 0;
+              if (((no_page >> u) & 1u) || e + tb >= cs.L) sb = 0;
+            }
+            s[k][0] = kv4_f16x2_e4m3(D == 256 ? __byte_perm(sa, sb, 0x0040) : sa | sb << 8);
+            if constexpr (D == 256) s[k][1] = kv4_f16x2_e4m3(__byte_perm(sa, sb, 0x0051));
+          }
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-            const float next = m - mref[nt][k] > 15.0f ? m - 7.0f : mref[nt][k];
-            const float corr = ex2(mref[nt][k] - next);
-            mref[nt][k] = next;
-            l[nt][k] *= corr;
+          for (int w = 0; w < VW; ++w) {
+            uint32_t lo[2][4], hi[2][4];  // even and odd channels of the word, entries (ta, tb) / (ta + 8, tb + 8)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              o[mt][nt][k] *= corr;
-              o[mt][nt][k + 2] *= corr;
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t p = code[2 * k][w], r = code[2 * k + 1][w];
+              kv4_f16_e2m1((p & 0x0f0f0f0fu) | ((r << 4) & 0xf0f0f0f0u), lo[k]);
+              kv4_f16_e2m1(((p >> 4) & 0x0f0f0f0fu) | (r & 0xf0f0f0f0u), hi[k]);
+              const uint32_t by = s[k][D == 256 ? w / 2 : 0];
+#pragma unroll
+              for (int b = 0; b < 4; ++b) {
+                lo[k][b] = mul2(lo[k][b], by);
+                hi[k][b] = mul2(hi[k][b], by);
+              }
             }
 #pragma unroll
-            for (int v = 0; v < 4; ++v) x[v >> 1][nt][k + 2 * (v & 1)] = fmaf(sc[v >> 1][nt][k + 2 * (v & 1)], f[nt][k], -next);
-          }
-      }
-      uint32_t pb[2][NT][2], pl[2][NT][2];
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float p[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) p[k] = ex2(x[u][nt][k]);
-          l[nt][0] += p[0] + p[2];
-          l[nt][1] += p[1] + p[3];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t hi = pack_f16(p[2 * k], p[2 * k + 1]);
-            pb[u][nt][k] = transpose8x8(hi);
-            if constexpr (TWO) {
-              const float2 back = kv4_unpack_f16(hi);
-              pl[u][nt][k] = transpose8x8(pack_f16(p[2 * k] - back.x, p[2 * k + 1] - back.y));
-            }
+              for (int nt = 0; nt < NT; ++nt) {
+                mma_f16(o[4 * w + b][nt], lo[0][b], hi[0][b], lo[1][b], hi[1][b], pb[u][nt][0], pb[u][nt][1]);
+                if constexpr (TWO) mma_f16(o[4 * w + b][nt], lo[0][b], hi[0][b], lo[1][b], hi[1][b], pl[u][nt][0], pl[u][nt][1]);
+              }
           }
         }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint8_t* gp = st + u * GROUP + 9 * D;
-        // the lane's entries: MMA columns 2 cq, 2 cq + 1, and 8 further
-        const int ta = 2 * cq + (cq & 1), tb = 2 * cq + 1 - (cq & 1);
-        constexpr int VW = D / 64;  // words of 8 channels per entry and lane: channels 8 VW g ..
-        uint32_t code[4][VW];
-        uint32_t s[2][D == 256 ? 2 : 1];  // scales of (ta, tb) and (ta + 8, tb + 8), per block of the lane
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint8_t* p = gp + ((k & 1 ? tb : ta) + 8 * (k >> 1)) * (D / 2) + g * 4 * VW;
-          if constexpr (VW == 1) code[k][0] = *reinterpret_cast<const uint32_t*>(p);
-          if constexpr (VW == 2) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
-            code[k][0] = v.x, code[k][1] = v.y;
-          }
-          if constexpr (VW == 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(p);
-            code[k][0] = v.x, code[k][1] = v.y, code[k][2] = v.z, code[k][3] = v.w;
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint8_t* p = gp + 8 * D + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
-          uint32_t sa, sb;
-          if constexpr (D == 256) {
-            sa = *reinterpret_cast<const uint16_t*>(p + (ta + 8 * k) * (D / 16));
-            sb = *reinterpret_cast<const uint16_t*>(p + (tb + 8 * k) * (D / 16));
-          } else {
-            sa = p[(ta + 8 * k) * (D / 16)];
-            sb = p[(tb + 8 * k) * (D / 16)];
-          }
-          if (!whole) {  // what lies behind the sequence may be anything, a scale's NaN too
-            const int e = e0 + 16 * u + 8 * k;
-            if (((no_page >> u) & 1u) || e + ta >= cs.L) sa = 0;
-            if (((no_page >> u) & 1u) || e + tb >= cs.L) sb = 0;
-          }
-          s[k][0] = kv4_f16x2_e4m3(D == 256 ? __byte_perm(sa, sb, 0x0040) : sa | sb << 8);
-          if constexpr (D == 256) s[k][1] = kv4_f16x2_e4m3(__byte_perm(sa, sb, 0x0051));
-        }
-#pragma unroll
-        for (int w = 0; w < VW; ++w) {
-          uint32_t lo[2][4], hi[2][4];  // even and odd channels of the word, entries (ta, tb) / (ta + 8, tb + 8)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t p = code[2 * k][w], r = code[2 * k + 1][w];
-            kv4_f16_e2m1((p & 0x0f0f0f0fu) | ((r << 4) & 0xf0f0f0f0u), lo[k]);
-            kv4_f16_e2m1(((p >> 4) & 0x0f0f0f0fu) | (r & 0xf0f0f0f0u), hi[k]);
-            const uint32_t by = s[k][D == 256 ? w / 2 : 0];
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              lo[k][b] = mul2(lo[k][b], by);
-              hi[k][b] = mul2(hi[k][b], by);
-            }
-          }
-#pragma unroll
-          for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_f16(o[4 * w + b][nt], lo[0][b], hi[0][b], lo[1][b], hi[1][b], pb[u][nt][0], pb[u][nt][1]);
-              if constexpr (TWO) mma_f16(o[4 * w + b][nt], lo[0][b], hi[0][b], lo[1][b], hi[1][b], pl[u][nt][0], pl[u][nt][1]);
-            }
-        }
-      }
+      };
+      if (__all_sync(0xffffffffu, e0 + TILE <= lim_min && no_page == 0)) compute(std::true_type{});
+      else compute(std::false_type{});
       __syncwarp();  // every lane is through with the stage
       if (left > 0) request(stage);
       if (++stage == STAGES) {

@@ -8,13 +8,14 @@
 //   warps 9-12   unpack them: a lane turns a word (8 channels) into 16 bytes of f16, exactly (code times scale has 6 significant
 //                bits), and stores them in the layout of an MMA operand (128-byte swizzle; neighbouring lanes write neighbouring
 //                16-byte chunks of a row, so that the stores of a quarter warp cover all banks)
-//   warp 13      S_g = Q_g K^T and O_g += P_g V (tcgen05.mma, M = 128, accumulators and P in tensor memory), for each Q tile g that
-//                has rows; the whole warp runs the loop and one elected lane issues
+//   warps 13, 14 S_g = Q_g K^T and O_g += P_g V (tcgen05.mma, M = 128, accumulators and P in tensor memory), a warp per Q tile g;
+//                the whole warp runs the loop and one elected lane issues
 //   warps 0-7    softmax: thread (g, r) owns row r of tile g and reads its 64 scores with tcgen05.ld.  P is formed relative to a
 //                reference maximum that is raised only by jumps of more than 2^8, kept 2^7 times as large (f16's range), and
 //                written to tensor memory in f16: one term for bf16 outputs, two otherwise, as in im_kv4_attn.cu.  q is scaled
 //                by a power of two per row so that bf16 fits f16.
-// Tensor memory (512 columns): S_g at 64 g, P_g at 128 + 64 g (32 columns a term), O_g at 256 + 128 g.
+// Tensor memory (512 columns): S_g at 64 g, P_g at 128 + 64 g (32 columns a term; one term: two buffers), O_g at 256 + 128 g.
+// With two buffers P needs no wait: S(j) is issued behind the product of tile j - 2, so who has seen S(j) may overwrite P(j - 2).
 // Every wait is bounded (IM_KV4_TIMEOUT).
 #include <math.h>
 
@@ -24,7 +25,7 @@ namespace {
 
 constexpr int KT = 64, ROWS = 128, QT = 2, BLOCK_ROWS = QT * ROWS;
 constexpr int UNPACK_WARPS = 4, UNPACK = UNPACK_WARPS * 32;
-constexpr int W_COPY = 8, W_UNPACK = 9, W_MMA = W_UNPACK + UNPACK_WARPS, THREADS = (W_MMA + 1) * 32;
+constexpr int W_COPY = 8, W_UNPACK = 9, W_MMA = W_UNPACK + UNPACK_WARPS, THREADS = (W_MMA + QT) * 32;
 constexpr int STAGES = 3, RAW = 5;
 constexpr int HALF_BYTES = KT * 128;  // 64 rows x 128 bytes (64 channels)
 constexpr int S_COL = 0, P_COL = 128, O_COL = 256, TMEM_COLS = 512;
@@ -36,7 +37,7 @@ struct Sizes {
 };
 
 struct Shared {
-  unsigned long long raw_full[RAW], raw_empty[RAW], full[STAGES], empty[STAGES], qfull[QT], sfull[QT], sempty[QT], pfull[QT], pvdone[QT], ofree[QT];
+  unsigned long long raw_full[RAW], raw_empty[RAW], full[STAGES], empty[STAGES], qfull[QT], sfull[QT], sempty[QT], pfull[QT], pvdone[QT], odone[QT], ofree[QT];
   long long cum[THREADS + 1], scan[THREADS / 32];
   int no_page[RAW];   // groups of a raw tile that have no page (bits)
   int hidden[STAGES]; // the same for the unpacked tile
@@ -46,18 +47,32 @@ struct Shared {
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// bounded; the whole warp waits, and gets one answer (what follows is collective)
+// Bounded; the whole warp waits, and gets one answer (what follows is collective).  NAP: nanoseconds between attempts, for
+// the warps that work ahead of the others: attempts take issue slots from the softmax warps (a third of all instructions
+// when every warp polled without a pause).
+__device__ __forceinline__ uint32_t mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done;
+}
+template <int NAP = 0>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
   uint32_t done = 0;
-  for (uint32_t it = 0; it < IM_WAIT_LIMIT && !done; ++it) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    if ((it & 63) == 63 && *abort_flag) break;
+#pragma unroll 1
+  for (uint32_t it = 0; it < IM_WAIT_LIMIT / 16; ++it) {
+#pragma unroll 1
+    for (int k = 0; k < 16 && !done; ++k) {
+      if (NAP) __nanosleep(NAP);
+      done = mbar_try(bar, parity);
+    }
+    if (done || *abort_flag) break;
   }
   return __all_sync(0xffffffffu, done);
 }
@@ -169,7 +184,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
     }
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&sh.full[s]), UNPACK);
-      mbar_init(smem_u32(&sh.empty[s]), 1);
+      mbar_init(smem_u32(&sh.empty[s]), QT);
     }
     for (int g = 0; g < QT; ++g) {
       mbar_init(smem_u32(&sh.qfull[g]), ROWS);
@@ -177,6 +192,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
       mbar_init(smem_u32(&sh.sempty[g]), ROWS);
       mbar_init(smem_u32(&sh.pfull[g]), ROWS);
       mbar_init(smem_u32(&sh.pvdone[g]), 1);
+      mbar_init(smem_u32(&sh.odone[g]), 1);
       mbar_init(smem_u32(&sh.ofree[g]), ROWS);
     }
     sh.abort = 0;
@@ -225,7 +241,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
             win_end = t + 32 / pieces;
           }
           const int r = n % RAW;
-          if (n >= RAW && !mbar_wait(smem_u32(&sh.raw_empty[r]), (uint32_t)((n / RAW - 1) & 1), abort_flag)) { ok = false; break; }
+          if (n >= RAW && !mbar_wait<200>(smem_u32(&sh.raw_empty[r]), (uint32_t)((n / RAW - 1) & 1), abort_flag)) { ok = false; break; }
           const int page = __shfl_sync(0xffffffffu, win, min(31, (t - win_base) * pieces + min(lane, pieces - 1)));
           const bool has = lane < pieces && (unsigned)page < (unsigned)c.n_pages;
           const int at = t * KT + lane * piece;
@@ -254,84 +270,89 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
         for (int t = g.tile; t < g.end; ++t, ++n) {
           const int r = n % RAW, s = n % STAGES;
           if (!mbar_wait(smem_u32(&sh.raw_full[r]), (uint32_t)((n / RAW) & 1), abort_flag)) { ok = false; break; }
-          if (n >= STAGES && !mbar_wait(smem_u32(&sh.empty[s]), (uint32_t)((n / STAGES - 1) & 1), abort_flag)) { ok = false; break; }
-          const uint8_t* src = s_packed + r * Z::TILE;
-          uint8_t* dst = s_kv + s * Z::STAGE + (word >> 3) * HALF_BYTES;
+          if (n >= STAGES && !mbar_wait<40>(smem_u32(&sh.empty[s]), (uint32_t)((n / STAGES - 1) & 1), abort_flag)) { ok = false; break; }
+          const uint8_t* codes = s_packed + r * Z::TILE + r0 * (D / 2) + 4 * word;
+          const uint8_t* scales = s_packed + r * Z::TILE + 8 * D + r0 * (D / 16) + (word >> 1);
+          uint8_t* dst = s_kv + s * Z::STAGE + (word >> 3) * HALF_BYTES + r0 * 128 + (((word & 7) ^ (r0 & 7)) << 4);
           const int none = *(volatile int*)&sh.no_page[r], seen = g.L - t * KT;  // rows from `seen` on hold anything
-          const bool whole = seen >= KT && none == 0;
+          const bool whole = __all_sync(0xffffffffu, seen >= KT && none == 0);
           if (ut == 0) sh.hidden[s] = none;
+          // (every offset below is a constant but for those of the lane)
+          auto unpack = [&](auto all) {
 #pragma unroll
-          for (int v = 0; v < 2; ++v)
+            for (int v = 0; v < 2; ++v)
 #pragma unroll
-            for (int p = 0; p < KT / STEP; ++p) {
-              const int row = r0 + p * STEP;
-              const uint8_t* gp = src + (row >> 4) * Z::GROUP + v * 9 * D;
-              const uint32_t code = *reinterpret_cast<const uint32_t*>(gp + (row & 15) * (D / 2) + 4 * word);
-              uint32_t sc = gp[8 * D + (row & 15) * (D / 16) + (word >> 1)];
-              if (!whole && (row >= seen || ((none >> (row >> 4)) & 1))) sc = 0;
-              sc = kv4_f16x2_e4m3(sc);
-              const uint32_t by = __byte_perm(sc, sc, 0x1010);
-              uint32_t x[4];
-              kv4_f16_e2m1(code, x);
-              *reinterpret_cast<uint4*>(dst + v * Z::KV + (row >> 3) * 1024 + (row & 7) * 128 + (((word & 7) ^ (row & 7)) << 4)) =
-                  make_uint4(mul2(x[0], by), mul2(x[1], by), mul2(x[2], by), mul2(x[3], by));
-            }
+              for (int p = 0; p < KT / STEP; ++p) {
+                const int group = p * STEP / 16, up = p * STEP % 16;  // row r0 + p STEP = row r0 + up of the group
+                const uint32_t code = *reinterpret_cast<const uint32_t*>(codes + group * Z::GROUP + v * 9 * D + up * (D / 2));
+                uint32_t sc = scales[group * Z::GROUP + v * 9 * D + up * (D / 16)];
+                if (!decltype(all)::value && (r0 + p * STEP >= seen || ((none >> group) & 1))) sc = 0;
+                sc = kv4_f16x2_e4m3(sc);
+                const uint32_t by = __byte_perm(sc, sc, 0x1010);
+                uint32_t x[4];
+                kv4_f16_e2m1(code, x);
+                *reinterpret_cast<uint4*>(dst + v * Z::KV + p * STEP * 128) = make_uint4(mul2(x[0], by), mul2(x[1], by), mul2(x[2], by), mul2(x[3], by));
+              }
+          };
+          if (whole) unpack(std::true_type{});
+          else unpack(std::false_type{});
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           mbar_arrive(smem_u32(&sh.full[s]));
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&sh.raw_empty[r]));
         }
       }
-    } else if (warp == W_MMA) {
-      // ---- products.  Order: S_0 S_1 of the first tile | S_0(j + 1) PV_0(j) S_1(j + 1) PV_1(j) | ...: the scores of the next
-      // tile are issued as soon as the softmax threads have read the last, ahead of the product that waits for their P.
+    } else if (warp >= W_MMA) {
+      // ---- products: a warp per Q tile, so that neither waits for the other's softmax.  The scores of the next tile are issued
+      // as soon as the softmax threads have read the last, ahead of the product that waits for their P.
+      const int x = warp - W_MMA;
       const uint32_t idesc_s = (1u << 4) | ((uint32_t)(KT >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
-      const uint32_t qa = smem_u32(s_q);
-      int n0 = 0, cnt[QT] = {}, segs[QT] = {};  // tiles before this segment; tiles / segments of each Q tile so far
+      const uint32_t qa = smem_u32(s_q) + x * Z::Q, kv = smem_u32(s_kv);
+      int n = 0, cnt = 0, segs = 0;  // tiles so far; tiles and segments of this Q tile
+      auto scores = [&](int m, int k, bool first) -> bool {  // tile m of the run, k of this Q tile
+        if (!mbar_wait(smem_u32(&sh.full[m % STAGES]), (uint32_t)((m / STAGES) & 1), abort_flag)) return false;
+        if (first && !mbar_wait(smem_u32(&sh.qfull[x]), (uint32_t)(segs & 1), abort_flag)) return false;
+        if (k >= 1 && !mbar_wait(smem_u32(&sh.sempty[x]), (uint32_t)((k - 1) & 1), abort_flag)) return false;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t ka = kv + (m % STAGES) * Z::STAGE;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          mma_ss(tmem + (uint32_t)(S_COL + x * KT), desc_sw128(qa + (ks >> 2) * (ROWS * 128) + (ks & 3) * 32, 16, 1024),
+                 desc_sw128(ka + (ks >> 2) * HALF_BYTES + (ks & 3) * 32, 16, 1024), idesc_s, ks ? 1u : 0u);
+        mma_commit(smem_u32(&sh.sfull[x]));
+        return true;
+      };
       while (ok && next_segment(a, w, t0, t1, &g)) {
-        const int nt = g.end - g.tile, qt = g.rows > ROWS ? 2 : 1;
-        auto issue_s = [&](int j, int x) -> bool {
-          const int s = (n0 + j) % STAGES, k = cnt[x] + j;
-          if (x == 0 && !mbar_wait(smem_u32(&sh.full[s]), (uint32_t)(((n0 + j) / STAGES) & 1), abort_flag)) return false;
-          if (j == 0 && !mbar_wait(smem_u32(&sh.qfull[x]), (uint32_t)(segs[x] & 1), abort_flag)) return false;
-          if (k >= 1 && !mbar_wait(smem_u32(&sh.sempty[x]), (uint32_t)((k - 1) & 1), abort_flag)) return false;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t ka = smem_u32(s_kv + s * Z::STAGE);
-#pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-            mma_ss(tmem + (uint32_t)(S_COL + x * KT), desc_sw128(qa + x * Z::Q + (ks >> 2) * (ROWS * 128) + (ks & 3) * 32, 16, 1024),
-                   desc_sw128(ka + (ks >> 2) * HALF_BYTES + (ks & 3) * 32, 16, 1024), idesc_s, ks ? 1u : 0u);
-          mma_commit(smem_u32(&sh.sfull[x]));
-          return true;
-        };
-        for (int x = 0; x < qt && ok; ++x) ok = issue_s(0, x);
-        for (int j = 0; j < nt && ok; ++j) {
-          const int s = (n0 + j) % STAGES;
-          const uint32_t va = smem_u32(s_kv + s * Z::STAGE) + Z::KV;
-          for (int x = 0; x < qt && ok; ++x) {
-            if (j + 1 < nt && !issue_s(j + 1, x)) { ok = false; break; }
-            if (!mbar_wait(smem_u32(&sh.pfull[x]), (uint32_t)((cnt[x] + j) & 1), abort_flag)) { ok = false; break; }
-            if (j == 0 && segs[x] > 0 && !mbar_wait(smem_u32(&sh.ofree[x]), (uint32_t)((segs[x] - 1) & 1), abort_flag)) { ok = false; break; }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-            for (int term = 0; term < (TWO ? 2 : 1); ++term)
-#pragma unroll
-              for (int ks = 0; ks < KT / 16; ++ks)
-                mma_ts(tmem + (uint32_t)(O_COL + x * 128), tmem + (uint32_t)(P_COL + 64 * x + 32 * term + 8 * ks),
-                       desc_sw128(va + ks * 2048, HALF_BYTES, 1024), idesc_o, (j | term | ks) ? 1u : 0u);
-            mma_commit(smem_u32(&sh.pvdone[x]));
+        const int nt = g.end - g.tile;
+        if (x * ROWS >= g.rows) {  // no rows: hand the stages on as they come
+          for (int j = 0; j < nt && ok; ++j, ++n) {
+            ok = mbar_wait(smem_u32(&sh.full[n % STAGES]), (uint32_t)((n / STAGES) & 1), abort_flag);
+            if (ok && lane == 0) mbar_arrive(smem_u32(&sh.empty[n % STAGES]));
           }
-          if (ok) mma_commit(smem_u32(&sh.empty[s]));
+          continue;
         }
-        for (int x = 0; x < qt; ++x) {
-          cnt[x] += nt;
-          ++segs[x];
+        ok = scores(n, cnt, true);
+        for (int j = 0; j < nt && ok; ++j, ++n, ++cnt) {
+          if (j + 1 < nt && !scores(n + 1, cnt + 1, false)) { ok = false; break; }
+          if (!mbar_wait(smem_u32(&sh.pfull[x]), (uint32_t)(cnt & 1), abort_flag)) { ok = false; break; }
+          if (j == 0 && segs > 0 && !mbar_wait(smem_u32(&sh.ofree[x]), (uint32_t)((segs - 1) & 1), abort_flag)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t va = kv + (n % STAGES) * Z::STAGE + Z::KV;
+#pragma unroll
+          for (int term = 0; term < (TWO ? 2 : 1); ++term)
+#pragma unroll
+            for (int ks = 0; ks < KT / 16; ++ks)
+              mma_ts(tmem + (uint32_t)(O_COL + x * 128), tmem + (uint32_t)(P_COL + 64 * x + 32 * (TWO ? term : cnt & 1) + 8 * ks),
+                     desc_sw128(va + ks * 2048, HALF_BYTES, 1024), idesc_o, (j | term | ks) ? 1u : 0u);
+          mma_commit(smem_u32(&sh.pvdone[x]));
+          if (j + 1 == nt) mma_commit(smem_u32(&sh.odone[x]));
+          mma_commit(smem_u32(&sh.empty[n % STAGES]));
         }
-        n0 += nt;
+        ++segs;
       }
       // (the last arrivals land before the block's memory is handed on)
-      if (ok) ok = mbar_wait(smem_u32(&sh.empty[(n0 - 1) % STAGES]), (uint32_t)(((n0 - 1) / STAGES) & 1), abort_flag);
+      if (ok) ok = mbar_wait(smem_u32(&sh.empty[(n - 1) % STAGES]), (uint32_t)(((n - 1) / STAGES) & 1), abort_flag);
     } else if (warp < 8) {
       // ---- softmax: warps 4 x .. 4 x + 3 own Q tile x, thread = row = lane of tensor memory
       const int x = warp >> 2, r = tid & (ROWS - 1);
@@ -339,7 +360,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
       const uint32_t t_s = tmem + lane_addr + (uint32_t)(S_COL + x * KT);
       const uint32_t t_p = tmem + lane_addr + (uint32_t)(P_COL + 64 * x);
       const uint32_t t_o = tmem + lane_addr + (uint32_t)(O_COL + 128 * x);
-      int n0 = 0, cnt = 0;
+      int n0 = 0, cnt = 0, segs = 0;
       while (ok && next_segment(a, w, t0, t1, &g)) {
         const int nt = g.end - g.tile;
         if (x * ROWS >= g.rows) {  // nothing for this Q tile
@@ -387,40 +408,45 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
           mbar_arrive(smem_u32(&sh.qfull[x]));
         }
         const float f = row_factor(a, g.h, ex);
-        float mref = NO_MAX, l = 0.f;
+        const int lim_min = __reduce_min_sync(0xffffffffu, there ? lim : g.L);
+        float mref = NO_MAX;
+        float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};  // the sum of p, in four parts
         for (int j = 0; j < nt; ++j) {
           const int k = cnt + j;
           if (!mbar_wait(smem_u32(&sh.sfull[x]), (uint32_t)(k & 1), abort_flag)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const int none = *(volatile int*)&sh.hidden[(n0 + j) % STAGES];
           float sv[KT];
           tmem_ld32(t_s, sv);
           tmem_ld32(t_s + 32, sv + 32);
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           mbar_arrive(smem_u32(&sh.sempty[x]));
           const int e0 = (g.tile + j) * KT;
-          const int none = *(volatile int*)&sh.hidden[(n0 + j) % STAGES];
-          if (e0 + KT > lim || none) {
+          if (e0 + KT > lim_min || none) {  // (the same for the whole warp; the tiles that need it are few)
 #pragma unroll
             for (int b = 0; b < KT; ++b)
               if (e0 + b >= lim || ((none >> (b >> 4)) & 1)) sv[b] = NEG_INF;
           }
           float m0 = sv[0], m1 = sv[1], m2 = sv[2], m3 = sv[3];
 #pragma unroll
-          for (int b = 4; b < KT; b += 4) {
-            m0 = fmaxf(m0, sv[b]);
-            m1 = fmaxf(m1, sv[b + 1]);
-            m2 = fmaxf(m2, sv[b + 2]);
-            m3 = fmaxf(m3, sv[b + 3]);
+          for (int b = 4; b < KT - 4; b += 8) {
+            m0 = max3(m0, sv[b], sv[b + 1]);
+            m1 = max3(m1, sv[b + 2], sv[b + 3]);
+            m2 = max3(m2, sv[b + 4], sv[b + 5]);
+            m3 = max3(m3, sv[b + 6], sv[b + 7]);
           }
-          const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * f;
+          m0 = max3(m0, sv[KT - 4], sv[KT - 3]);
+          m1 = max3(m1, sv[KT - 2], sv[KT - 1]);
+          const float top = max3(m0, m1, fmaxf(m2, m3)) * f;
           const bool raise = top - mref > 15.0f;
           bool pv_waited = false;
           if (__any_sync(0xffffffffu, raise)) {
             const float next = raise ? top - 7.0f : mref;
             const float corr = ex2(mref - next);
             mref = next;
-            l *= corr;
-            if (j >= 1) {  // O holds the products up to tile j - 1: wait for the last one, then scale the row
+#pragma unroll
+            for (int b = 0; b < 2; ++b) l2[b].x *= corr, l2[b].y *= corr;
+            if (j >= 1) {  // O holds the products up to tile j - 1 (that of j - 2 is complete): wait for the last one, then scale the row
               if (!mbar_wait(smem_u32(&sh.pvdone[x]), (uint32_t)((k - 1) & 1), abort_flag)) { ok = false; break; }
               pv_waited = true;
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -447,19 +473,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
             uint32_t hi[16], lo[16];
 #pragma unroll
             for (int b = 0; b < 16; ++b) {
-              const float p0 = ex2(fmaf(sv[32 * hf + 2 * b], f, -mref)), p1 = ex2(fmaf(sv[32 * hf + 2 * b + 1], f, -mref));
-              l += p0 + p1;
-              hi[b] = pack_f16(p0, p1);
+              const float2 e = fma2(make_float2(sv[32 * hf + 2 * b], sv[32 * hf + 2 * b + 1]), make_float2(f, f), make_float2(-mref, -mref));
+              const float2 p = make_float2(ex2(e.x), ex2(e.y));
+              l2[b & 1] = add2(l2[b & 1], p);
+              hi[b] = pack_f16(p.x, p.y);
               if constexpr (TWO) {
                 const float2 back = kv4_unpack_f16(hi[b]);
-                lo[b] = pack_f16(p0 - back.x, p1 - back.y);
+                lo[b] = pack_f16(p.x - back.x, p.y - back.y);
               }
             }
-            if (hf == 0 && j >= 1 && !pv_waited) {  // P is single buffered: the product of tile j - 1 has to be through with it
+            if (TWO && hf == 0 && j >= 1 && !pv_waited) {  // one buffer: the product of tile j - 1 has to be through with it
               if (!mbar_wait(smem_u32(&sh.pvdone[x]), (uint32_t)((k - 1) & 1), abort_flag)) { ok = false; break; }
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-            tmem_st16(t_p + (uint32_t)(16 * hf), hi);
+            tmem_st16(t_p + (uint32_t)(16 * hf + (TWO ? 0 : 32 * (k & 1))), hi);
             if constexpr (TWO) tmem_st16(t_p + (uint32_t)(32 + 16 * hf), lo);
           }
           if (!ok) break;
@@ -470,9 +497,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
         if (!ok) break;
         cnt += nt;
         n0 += nt;
-        if (!mbar_wait(smem_u32(&sh.pvdone[x]), (uint32_t)((cnt - 1) & 1), abort_flag)) { ok = false; break; }
+        // (a barrier of its own: with two buffers up to two products are outstanding here, and pvdone's parity cannot tell them apart)
+        if (!mbar_wait(smem_u32(&sh.odone[x]), (uint32_t)(segs & 1), abort_flag)) { ok = false; break; }
+        ++segs;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         // ---- the segment's result
+        const float l = (l2[0].x + l2[1].x) + (l2[0].y + l2[1].y);
         const size_t at = (size_t)(g.first + token) * a.H + head;
         const float inv = l == 0.f ? 0.f : kv4_pow2(kv4_exp(c.v_exp, g.h)) / l;
         OutT* op = out + at * D;
