@@ -76,6 +76,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   int workers, per;
   const Deal deal = deal_line<ROWS, TILE, THREADS>(a, s_cum, s_scan, (long long)gridDim.x * WARPS, &workers, &per);
+  empty_rows<D>(a, out, lse);
   const int worker = warp * gridDim.x + blockIdx.x;  // neighbours in the line sit on different SMs
   if (worker >= workers) return;
   const long long t0 = worker * deal.q + min((long long)worker, deal.rest), t1 = t0 + deal.q + (worker < deal.rest ? 1 : 0);
@@ -468,12 +469,12 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
 
 // ------------------------------------------------------------------ host side
 size_t workspace(const Kv4& c, long long rows, int nt, uint8_t* base, AttnWs* ws) {
-  const size_t cum = 256, part = cum + kv4_align(8 * (size_t)c.n_seqs);
-  if (ws) *ws = {(Deal*)base, (long long*)(base + cum), (float*)(base + part)};
   // no more workers than tiles
   const double tiles = (double)c.n_seqs * ((double)c.max_pages * c.ps / TILE + 1) * c.Hkv * (double)((rows + 8 * nt - 1) / (8 * nt));
   const int most = MOST_SMS * warps_of(c.d, nt);
   const size_t workers = tiles < most ? (size_t)tiles : (size_t)most;
+  const size_t cum = 256, part = cum + kv4_align(8 * (size_t)c.n_seqs);
+  if (ws) *ws = {(Deal*)base, (long long*)(base + cum), nullptr, (float*)(base + part)};
   return part + kv4_align(2 * workers * 8 * nt * (c.d + 4) * 4);
 }
 
@@ -490,7 +491,7 @@ cudaError_t launch(const AttnArgs& a, const void* q, void* out, float* lse, int 
   }
   cudaError_t e = kv4_launch(k_kv4_stream<D, NT, TWO, T, OutT>, dim3(grid), warps_of(D, NT) * 32, smem, s, false, a, (const T*)q, (OutT*)out, lse);
   if (e == cudaSuccess)
-    e = kv4_launch(k_kv4_merge<D, 8 * NT, TILE, OutT>, dim3(a.n_tokens, a.H), MERGE_THREADS, 0, s, true, a, (OutT*)out, lse);
+    e = kv4_launch(k_kv4_join_tokens<D, 8 * NT, TILE, 4, OutT>, dim3(a.n_tokens, a.H), 4 * 32, 0, s, true, a, (OutT*)out, lse);
   return e;
 }
 

@@ -3,7 +3,7 @@
 //
 // The entries of all items (sequence, KV head, row block) form one line of tiles, sequence-major; a worker gets an equal run
 // of it whatever the lengths are, which the device alone knows.  An item that one worker runs through is written by it; of
-// the others the workers leave (sum of p v, reference maximum, sum of p) in the workspace, and k_kv4_merge adds those up in
+// the others the workers leave (sum of p v, reference maximum, sum of p) in the workspace, and k_kv4_join adds those up in
 // order of the workers: results do not depend on timing.
 #pragma once
 #include <type_traits>
@@ -12,11 +12,18 @@
 
 struct Deal {
   long long q, rest;  // the first `rest` workers get q + 1 tiles, the others q
+  int workers;
+};
+struct Piece {  // of a worker whose run begins inside an item: that item
+  long long base;  // its first tile in the line; -1: the run begins with an item
+  int tiles, rows;
+  int first_row, seq_first, h, pad;  // row block's first row, the sequence's first query token, KV head
 };
 struct AttnWs {
   Deal* deal;
-  long long* cum;  // [n_seqs] tiles ahead of the sequence
-  float* part;     // [2 * workers][ROWS][D + 4]
+  long long* cum;  // [n_seqs] tiles ahead of the sequence (few rows: joined by query token), or
+  Piece* piece;    // [workers] (many rows: joined by worker)
+  float* part;   // [2 * workers][ROWS][D + 4]
 };
 struct AttnArgs {
   Kv4 c;
@@ -40,7 +47,6 @@ namespace {
 constexpr float NEG_INF = -__builtin_huge_valf();
 constexpr float NO_MAX = -1e30f;  // reference maximum of a row that has seen nothing
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int MERGE_THREADS = 128;
 constexpr int MOST_SMS = 160;     // workspaces are sized for this many; a grid never has more CTAs
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -158,16 +164,33 @@ __device__ __forceinline__ Deal deal_line(const AttnArgs& a, long long* s_cum, l
   const long long total = s_cum[THREADS];
   *workers = (int)min(most, max(1ll, total));
   *per_ = per;
-  const Deal d = {total / *workers, total % *workers};
+  const Deal d = {total / *workers, total % *workers, *workers};
   if (blockIdx.x == 0) {
     if (tid == 0) *a.ws.deal = d;
     long long at = s_cum[tid];
-    for (int i = tid * per; i < min(n, tid * per + per); ++i) {
-      a.ws.cum[i] = at;
-      at += work_of(a, seq_of<ROWS, TILE>(a, i));
-    }
+    if (a.ws.cum)
+      for (int i = tid * per; i < min(n, tid * per + per); ++i) {
+        a.ws.cum[i] = at;
+        at += work_of(a, seq_of<ROWS, TILE>(a, i));
+      }
   }
   return d;
+}
+// rows of sequences that hold nothing: zeros, and no sum.  The sequences go round the CTAs.
+template <int D, typename OutT>
+__device__ __forceinline__ void empty_rows(const AttnArgs& a, OutT* out, float* lse) {
+  for (int i = blockIdx.x; i < a.c.n_seqs; i += gridDim.x) {
+    if (a.lens[i] > 0) continue;
+    int first, nq;
+    queries_of(a, i, &first, &nq);
+    const size_t at = (size_t)first * a.H, n = (size_t)nq * a.H;
+    for (size_t x = threadIdx.x; x < n * (D / 8); x += blockDim.x) {
+      const float zero[8] = {};
+      put8(out + at * D + 8 * x, zero);
+    }
+    if (lse)
+      for (size_t x = threadIdx.x; x < n; x += blockDim.x) lse[at + x] = NEG_INF;
+  }
 }
 // the sequence that tile t (< total) of the line lies in, and the tile's place in it
 template <int ROWS, int TILE, int THREADS>
@@ -188,38 +211,30 @@ __device__ __forceinline__ int find_tile(const AttnArgs& a, const long long* s_c
   }
 }
 
-// Joins the partial results of the items that several warps share, and writes the rows that see nothing.  Block = (query token,
-// query head); its warps take the partial results in turn, so that all of them are asked for at once.
-template <int D, int ROWS, int TILE, typename OutT>
-__global__ void __launch_bounds__(MERGE_THREADS) k_kv4_merge(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
-  constexpr int CH = D / 32, WARPS = MERGE_THREADS / 32;
-  __shared__ float s_acc[WARPS][D], s_m[WARPS], s_l[WARPS];
-  const int t = blockIdx.x, head = blockIdx.y, h = head / a.G, j = head % a.G, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int i = kv4_find(a.cu, a.c.n_seqs, t);
-  if (i < 0) return;
-  const Seq s = seq_of<ROWS, TILE>(a, i);
-  const float vup = kv4_pow2(kv4_exp(a.c.v_exp, h));
-  const int r = (t - s.first) * a.G + j;
+// ---- joining the partial results of an item that workers w0 .. w1 share
+constexpr int JOIN_WARPS = 8;
+__device__ __forceinline__ int worker_of(const Deal& d, long long x) {  // (of tile x)
+  const long long big = d.rest * (d.q + 1);
+  if (((big | x) >> 31) == 0) {
+    const unsigned q = (unsigned)d.q;
+    return x < big ? (int)((unsigned)x / (q + 1)) : (int)d.rest + (int)((unsigned)(x - big) / q);
+  }
+  return (int)(x < big ? x / (d.q + 1) : d.rest + (x - big) / d.q);
+}
+// Row r of the item, by PER warps of the block (they share its results, so that all of them are asked for at once); `at`: the
+// row of out and lse.  The whole block calls it with the same w0, w1 where PER > 1.
+template <int D, int ROWS, int PER, typename OutT>
+__device__ __forceinline__ void join_row(const AttnArgs& a, int w0, int w1, int r, bool there, int h, size_t at, OutT* out, float* lse) {
+  constexpr int CH = D / 32;
+  __shared__ float s_acc[JOIN_WARPS][D], s_m[JOIN_WARPS], s_l[JOIN_WARPS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % PER;
   float acc[CH], total = 0.f, m = NO_MAX;
 #pragma unroll
   for (int k = 0; k < CH; ++k) acc[k] = 0.f;
-  pdl_wait();
-  if (s.tiles) {
-    const Deal deal = *a.ws.deal;
-    const long long base = a.ws.cum[i] + ((long long)h * s.rb + r / ROWS) * s.tiles;
-    auto worker_of = [&](long long x) {
-      const long long big = deal.rest * (deal.q + 1);
-      if (((big | x) >> 31) == 0) {
-        const unsigned q = (unsigned)deal.q;
-        return x < big ? (int)((unsigned)x / (q + 1)) : (int)deal.rest + (int)((unsigned)(x - big) / q);
-      }
-      return (int)(x < big ? x / (deal.q + 1) : deal.rest + (x - big) / deal.q);
-    };
-    const int w0 = worker_of(base), w1 = worker_of(base + s.tiles - 1);
-    if (w0 == w1) return;  // written where it was computed
-    // worker w's result: its run began ahead of the item, but for the first one's
-    const float* part = a.ws.part + (size_t)(r % ROWS) * (D + 4);
-    for (int b = w0 + warp * 32; b <= w1; b += MERGE_THREADS) {
+  if (there) {
+    // worker x's result: its run began ahead of the item, but for the first one's
+    const float* part = a.ws.part + (size_t)r * (D + 4);
+    for (int b = w0 + sub * 32; b <= w1; b += PER * 32) {
       const int mine = b + lane;
       float2 ml = make_float2(NO_MAX, 0.f);
       if (mine <= w1) ml = *reinterpret_cast<const float2*>(part + (size_t)(2 * mine + (mine == w0 ? 1 : 0)) * (ROWS * (D + 4)) + D);
@@ -238,45 +253,45 @@ __global__ void __launch_bounds__(MERGE_THREADS) k_kv4_merge(const AttnArgs a, O
       const int n = min(32, w1 + 1 - b);
 #pragma unroll 8
       for (int x = 0; x < n; ++x) {
-        const int w = b + x;
+        const int y = b + x;
         const float by = __shfl_sync(0xffffffffu, e, x);
-        const float* p = part + (size_t)(2 * w + (w == w0 ? 1 : 0)) * (ROWS * (D + 4));
+        const float* q = part + (size_t)(2 * y + (y == w0 ? 1 : 0)) * (ROWS * (D + 4));
         if constexpr (CH == 2) {
-          const float2 v = *reinterpret_cast<const float2*>(p + 2 * lane);
+          const float2 v = *reinterpret_cast<const float2*>(q + 2 * lane);
           acc[0] = fmaf(v.x, by, acc[0]), acc[1] = fmaf(v.y, by, acc[1]);
         } else {
 #pragma unroll
           for (int k = 0; k < CH; k += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(p + CH * lane + k);
+            const float4 v = *reinterpret_cast<const float4*>(q + CH * lane + k);
             acc[k] = fmaf(v.x, by, acc[k]), acc[k + 1] = fmaf(v.y, by, acc[k + 1]);
             acc[k + 2] = fmaf(v.z, by, acc[k + 2]), acc[k + 3] = fmaf(v.w, by, acc[k + 3]);
           }
         }
       }
     }
-    if (w1 - w0 >= 32) {  // (the same for the whole block)
+  }
+  if (PER > 1 && w1 - w0 >= 32) {  // (the same for the whole block)
 #pragma unroll
-      for (int k = 0; k < CH; ++k) s_acc[warp][CH * lane + k] = acc[k];
-      if (lane == 0) s_m[warp] = m, s_l[warp] = total;
-      __syncthreads();
-      if (warp) return;
+    for (int k = 0; k < CH; ++k) s_acc[warp][CH * lane + k] = acc[k];
+    if (lane == 0) s_m[warp] = m, s_l[warp] = total;
+    __syncthreads();
+    if (sub == 0) {
 #pragma unroll
-      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_m[w]);
+      for (int x = 1; x < PER; ++x) m = fmaxf(m, s_m[warp + x]);
       total = 0.f;
 #pragma unroll
       for (int k = 0; k < CH; ++k) acc[k] = 0.f;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const float by = ex2(s_m[w] - m);
-        total = fmaf(s_l[w], by, total);
+      for (int x = 0; x < PER; ++x) {
+        const float by = ex2(s_m[warp + x] - m);
+        total = fmaf(s_l[warp + x], by, total);
 #pragma unroll
-        for (int k = 0; k < CH; ++k) acc[k] = fmaf(s_acc[w][CH * lane + k], by, acc[k]);
+        for (int k = 0; k < CH; ++k) acc[k] = fmaf(s_acc[warp + x][CH * lane + k], by, acc[k]);
       }
     }
   }
-  if (warp) return;
-  const size_t at = (size_t)t * a.H + head;
-  const float inv = total == 0.f ? 0.f : vup / total;
+  if (!there || sub) return;
+  const float inv = total == 0.f ? 0.f : kv4_pow2(kv4_exp(a.c.v_exp, h)) / total;
   OutT* dst = out + at * D + CH * lane;
 #pragma unroll
   for (int k = 0; k < CH; k += 2) {
@@ -284,6 +299,36 @@ __global__ void __launch_bounds__(MERGE_THREADS) k_kv4_merge(const AttnArgs a, O
     else *reinterpret_cast<float2*>(dst + k) = make_float2(acc[k] * inv, acc[k + 1] * inv);
   }
   if (lse && lane == 0) lse[at] = total == 0.f ? NEG_INF : (m + log2f(total)) * LN2;
+}
+
+// Few rows: block = (query token, heads), PER warps per query head.  A row that sees nothing is written where it was found.
+template <int D, int ROWS, int TILE, int PER, typename OutT>
+__global__ void __launch_bounds__(PER * 32) k_kv4_join_tokens(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
+  const int t = blockIdx.x, head = blockIdx.y, h = head / a.G;
+  const int i = kv4_find(a.cu, a.c.n_seqs, t);
+  if (i < 0) return;
+  const Seq s = seq_of<ROWS, TILE>(a, i);
+  const int r = (t - s.first) * a.G + head % a.G;
+  pdl_wait();
+  const Deal deal = *a.ws.deal;
+  if (!s.tiles) return;
+  const long long base = a.ws.cum[i] + ((long long)h * s.rb + r / ROWS) * s.tiles;
+  const int w0 = worker_of(deal, base), w1 = worker_of(deal, base + s.tiles - 1);
+  if (w0 == w1) return;  // written where it was computed
+  join_row<D, ROWS, PER>(a, w0, w1, r % ROWS, true, h, (size_t)t * a.H + head, out, lse);
+}
+// Many rows: block (w, y) = the item that worker w + 1's run begins inside, if w + 1 is the second worker on it (each shared item
+// has one); a warp per row, JOIN_WARPS rows by y.
+template <int D, int ROWS, typename OutT>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) k_kv4_join_workers(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
+  const int w = blockIdx.x + 1, r = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
+  pdl_wait();
+  const Deal deal = *a.ws.deal;
+  if (w >= deal.workers || deal.q == 0) return;
+  const Piece p = a.ws.piece[w];
+  if (p.base < 0 || (w - 1) * deal.q + min((long long)w - 1, deal.rest) > p.base || r >= p.rows) return;
+  const int row = p.first_row + r;
+  join_row<D, ROWS, 1>(a, w - 1, worker_of(deal, p.base + p.tiles - 1), r, true, p.h, (size_t)(p.seq_first + row / a.G) * a.H + p.h * a.G + row % a.G, out, lse);
 }
 
 }  // namespace

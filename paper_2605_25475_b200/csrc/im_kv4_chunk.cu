@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
   const uint32_t tmem = sh.tmem;
   const int worker = blockIdx.x;
   const long long t0 = worker * deal.q + min((long long)worker, deal.rest), t1 = t0 + deal.q + (worker < deal.rest ? 1 : 0);
+  empty_rows<D>(a, out, lse);
   bool ok = true;
   if (worker < workers && t0 < t1) {
     Walk w;
@@ -222,6 +223,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
     w.rb = item % w.s.rb;
     w.todo = (int)(t1 - t0);
     Segment g;
+    if (tid == 0) {  // what the run begins with
+      Walk v = w;
+      next_segment(a, v, t0, t1, &g);
+      a.ws.piece[worker] = {g.base < t0 ? g.base : -1, w.s.tiles, g.rows, g.row0, g.first, g.h, 0};
+    }
 
     if (warp == W_COPY) {
       // ---- packed tiles: 64 entries are 4, 2 or 1 pieces of pages
@@ -556,8 +562,8 @@ cudaError_t launch(const AttnArgs& a, const void* q, void* out, float* lse, int 
     *done = true;
   }
   cudaError_t e = kv4_launch(k_kv4_chunk<D, TWO, T, OutT>, dim3(grid), THREADS, Sizes<D>::BYTES, s, false, a, (const T*)q, (OutT*)out, lse);
-  if (e == cudaSuccess)
-    e = kv4_launch(k_kv4_merge<D, BLOCK_ROWS, KT, OutT>, dim3(a.n_tokens, a.H), MERGE_THREADS, 0, s, true, a, (OutT*)out, lse);
+  if (e == cudaSuccess && grid > 1)
+    e = kv4_launch(k_kv4_join_workers<D, BLOCK_ROWS, OutT>, dim3(grid - 1, BLOCK_ROWS / JOIN_WARPS), JOIN_WARPS * 32, 0, s, true, a, (OutT*)out, lse);
   return e;
 }
 template <int D>
@@ -569,8 +575,8 @@ cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* 
 }  // namespace
 
 size_t kv4_chunk_workspace(const Kv4& c, uint8_t* base, AttnWs* ws) {
-  const size_t cum = 256, part = cum + kv4_align(8 * (size_t)c.n_seqs);
-  if (ws) *ws = {(Deal*)base, (long long*)(base + cum), (float*)(base + part)};
+  const size_t piece = 256, part = piece + kv4_align(sizeof(Piece) * MOST_SMS);
+  if (ws) *ws = {(Deal*)base, nullptr, (Piece*)(base + piece), (float*)(base + part)};
   return part + kv4_align(2 * (size_t)MOST_SMS * BLOCK_ROWS * (c.d + 4) * 4);
 }
 cudaError_t kv4_launch_chunk(const AttnArgs& a, int dtype, int out_f32, const void* q, void* out, float* lse, int grid, cudaStream_t s) {
