@@ -26,28 +26,30 @@ struct PlanWs {
   int32_t* info;  // [n_seqs] append: the shared last page whose tokens are copied, or -1; compact: pages that stay
   int32_t* cnt;   // [n_seqs] compact: survivors, or -1 for a row that is out of order
   int32_t* list;  // [list_max] the free pages in ascending order
+  int32_t* goff;  // [n_seqs + 1] compact: groups of 16 survivors to move, ahead of the sequence
   int32_t* src;   // [n_seqs][cap] compact: page * page_size + slot of the survivors
   int list_max, cap;
 };
 
-__device__ __forceinline__ long long warp_scan_incl(long long v, int lane) {
+template <typename N>
+__device__ __forceinline__ N warp_scan_incl(N v, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long u = __shfl_up_sync(0xffffffffu, v, o);
+    const N u = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += u;
   }
   return v;
 }
 // exclusive scan over the block; *total receives the block's sum
-template <int WARPS>
-__device__ __forceinline__ long long block_scan(long long v, long long* s_warp, long long* total) {
+template <int WARPS, typename N>
+__device__ __forceinline__ N block_scan(N v, N* s_warp, N* total) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long incl = warp_scan_incl(v, lane);
+  const N incl = warp_scan_incl(v, lane);
   __syncthreads();  // (the previous scan's readers are through with s_warp)
   if (lane == 31) s_warp[warp] = incl;
   __syncthreads();
   if (warp == 0) {
-    const long long w = warp_scan_incl(lane < WARPS ? s_warp[lane] : 0, lane);
+    const N w = warp_scan_incl(lane < WARPS ? s_warp[lane] : (N)0, lane);
     if (lane < WARPS) s_warp[lane] = w;
   }
   __syncthreads();
@@ -80,11 +82,11 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
   pdl_release();
   if (MODE == PLAN_COMPACT) pdl_wait();  // (the scan kernel's counts)
   // ---- what each sequence needs
-  long long total = 0;
+  long long total = 0, moves = 0;
   bool bad = false, full = false;
   for (int base = 0; base < c.n_seqs; base += PLAN_THREADS) {
     const int i = base + tid;
-    int need = 0, info = MODE == PLAN_APPEND ? -1 : 0;
+    int need = 0, move = 0, info = MODE == PLAN_APPEND ? -1 : 0;
     if (i < c.n_seqs) {
       const int L = from.lens[i];
       if (MODE == PLAN_APPEND) {
@@ -107,18 +109,27 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
       } else {
         const int cnt = ws.cnt[i];
         if (cnt < 0) bad = true;
-        else need = (cnt + c.ps - 1) / c.ps - ws.info[i];
+        else {
+          need = (cnt + c.ps - 1) / c.ps - ws.info[i];
+          move = max(0, (cnt - ws.info[i] * c.ps + 15) >> 4);
+        }
       }
     }
     long long chunk;
-    const long long before = block_scan<PLAN_WARPS>(need, s_warp, &chunk);
+    const long long before = block_scan<PLAN_WARPS>((long long)need, s_warp, &chunk);
     if (rank == 0 && i < c.n_seqs) {
       const long long o = total + before;
       ws.off[i] = (int)(o < 0x7fffffff ? o : 0x7fffffff);
       if (MODE == PLAN_APPEND) ws.info[i] = info;
     }
     total += chunk;
+    if (MODE == PLAN_COMPACT) {
+      const long long ahead = block_scan<PLAN_WARPS>((long long)move, s_warp, &chunk);
+      if (rank == 0 && i < c.n_seqs) ws.goff[i] = (int)(moves + ahead);
+      moves += chunk;
+    }
   }
+  if (MODE == PLAN_COMPACT && rank == 0 && tid == 0) ws.goff[c.n_seqs] = (int)moves;
   bad = __syncthreads_or(bad);
   full = __syncthreads_or(full);
   // ---- free pages of this CTA's share, in runs per warp
@@ -249,17 +260,18 @@ __device__ __forceinline__ float2 two_floats<__half>(uint32_t v) {
   return kv4_unpack_f16(v);
 }
 
-// One thread per block of 16 channels; grid.y = (head, keys / values), grid.x over (token, block): a warp reads whole rows
-// and writes the code rows of neighbouring tokens of one head, which lie side by side.  The rows of the grid behind those
-// copy the tokens of shared last pages.  The loads and the quantiser run ahead of the wait for the plan.
+// One thread per block of 16 channels, keys and values; grid.y = head, grid.x over (token, block): a warp reads whole rows and
+// writes the code rows of neighbouring tokens of one head, which lie side by side.  The rows of the grid behind those copy
+// the tokens of shared last pages.  The loads run ahead of the wait for the plan, and the lookups in its map (two round
+// trips) ahead of the quantiser.
 constexpr int STORE_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(STORE_THREADS)
 k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, const T* __restrict__ k, long long k_stride,
             const T* __restrict__ v, long long v_stride, int n_tokens, const int32_t* __restrict__ cu, PlanWs ws) {
-  const int h = blockIdx.y >> 1, which = blockIdx.y & 1;
+  const int h = blockIdx.y;
   if (h >= c.Hkv) {  // (sequence, head) by (sequence, head)
-    const int cow = (blockIdx.y - 2 * c.Hkv) * gridDim.x + blockIdx.x, step = (gridDim.y - 2 * c.Hkv) * gridDim.x;
+    const int cow = (blockIdx.y - c.Hkv) * gridDim.x + blockIdx.x, step = (gridDim.y - c.Hkv) * gridDim.x;
     pdl_wait();
     if (!*ws.ok) return;
     for (int task = cow; task < c.n_seqs * c.Hkv; task += step) {
@@ -289,17 +301,27 @@ k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict_
   }
   const int lg = c.d == 64 ? 2 : c.d == 128 ? 3 : 4;  // log2 of the blocks of a row
   const int idx = blockIdx.x * STORE_THREADS + threadIdx.x, blk = idx & ((1 << lg) - 1), t = idx >> lg;
+  uint4 in[4] = {};
   int i = -1;
-  uint2 codes = make_uint2(0u, 0u);
-  uint8_t scale = 0;
   if (t < n_tokens) {
-    const uint4* src = reinterpret_cast<const uint4*>((which ? v + t * v_stride : k + t * k_stride) + (size_t)h * c.d + blk * 16);
-    const uint4 a = src[0], b = src[1];
-    const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const uint4* ks = reinterpret_cast<const uint4*>(k + t * k_stride + (size_t)h * c.d + blk * 16);
+    const uint4* vs = reinterpret_cast<const uint4*>(v + t * v_stride + (size_t)h * c.d + blk * 16);
+    in[0] = ks[0], in[1] = ks[1], in[2] = vs[0], in[3] = vs[1];
     i = kv4_find(cu, c.n_seqs, t);
+  }
+  pdl_wait();
+  if (i < 0) return;
+  const int ok = *ws.ok, slot = lens[i] - (cu ? cu[i + 1] - t : 1);
+  const int page = ok && slot >= 0 && slot / c.ps < c.max_pages ? table[(size_t)i * c.max_pages + slot / c.ps] : -1;
+  bool odd = false;
+  uint2 codes[2];
+  uint8_t scale[2];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const uint4 a = in[2 * which], b = in[2 * which + 1];
+    const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     const float down = kv4_pow2(-kv4_exp(which ? c.v_exp : c.k_exp, h));
     float x[16];
-    bool odd = false;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const float2 f = two_floats<T>(raw[q]);
@@ -307,18 +329,16 @@ k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict_
       x[2 * q] = f.x == f.x ? f.x * down : 0.f;
       x[2 * q + 1] = f.y == f.y ? f.y * down : 0.f;
     }
-    codes = quantise16(x, &scale);
-    if (odd && i >= 0) atomicOr(c.status, IM_KV4_NONFINITE);
+    codes[which] = quantise16(x, &scale[which]);
   }
-  pdl_wait();
-  if (i < 0 || !*ws.ok) return;
-  const int slot = lens[i] - (cu ? cu[i + 1] - t : 1);
-  const int page = table[(size_t)i * c.max_pages + slot / c.ps];
-  if (page < 0 || page >= c.n_pages) return;  // (flagged by the plan)
+  if (odd) atomicOr(c.status, IM_KV4_NONFINITE);
+  if (page < 0 || page >= c.n_pages) return;  // (the call is not made, as the plan has flagged)
   const int at = slot % c.ps;
   uint8_t* g = kv4_group(c, page, h, at >> 4);
-  *reinterpret_cast<uint2*>(g + (which ? kv4_vc(c.d, at & 15) : kv4_kc(c.d, at & 15)) + 8 * blk) = codes;
-  g[(which ? kv4_vs(c.d, at & 15) : kv4_ks(c.d, at & 15)) + blk] = scale;
+  *reinterpret_cast<uint2*>(g + kv4_kc(c.d, at & 15) + 8 * blk) = codes[0];
+  g[kv4_ks(c.d, at & 15) + blk] = scale[0];
+  *reinterpret_cast<uint2*>(g + kv4_vc(c.d, at & 15) + 8 * blk) = codes[1];
+  g[kv4_vs(c.d, at & 15) + blk] = scale[1];
 }
 
 // ------------------------------------------------------------------ gather
@@ -448,7 +468,7 @@ k_kv4_fork(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ pa
 // sequence, 16 flags per thread and round.
 __global__ void __launch_bounds__(SCAN_THREADS)
 k_kv4_scan(Kv4 c, im_kv4_map from, const uint8_t* __restrict__ keep, int keep_stride, PlanWs ws) {
-  __shared__ long long s_warp[SCAN_THREADS / 32];
+  __shared__ int s_warp[SCAN_THREADS / 32];
   __shared__ int s_hole;
   pdl_release();
   const int i = blockIdx.x, tid = threadIdx.x;
@@ -481,15 +501,15 @@ k_kv4_scan(Kv4 c, im_kv4_map from, const uint8_t* __restrict__ keep, int keep_st
       const uint32_t all = L - t0 >= 16 ? 0xffffu : (1u << (L - t0)) - 1u;
       if (flags != all && hole == L) hole = t0 + __ffs(~flags & all) - 1;
     }
-    long long chunk;
-    int at = done + (int)block_scan<SCAN_THREADS / 32>(__popc(flags), s_warp, &chunk);
+    int chunk;
+    int at = done + block_scan<SCAN_THREADS / 32>(__popc(flags), s_warp, &chunk);
     if (flags) {  // 16 entries starting at a multiple of 16 lie in one page
       const int page = table[t0 / c.ps];
       if (page < 0 || page >= c.n_pages) bad = true;
       const int r0 = page * c.ps + t0 % c.ps;
       for (uint32_t m = flags; m; m &= m - 1) ws.src[(size_t)i * ws.cap + at++] = r0 + __ffs(m) - 1;
     }
-    done += (int)chunk;
+    done += chunk;
   }
   bad = __syncthreads_or(bad);
   if (hole < L) atomicMin(&s_hole, hole);
@@ -500,55 +520,72 @@ k_kv4_scan(Kv4 c, im_kv4_map from, const uint8_t* __restrict__ keep, int keep_st
   }
 }
 
-// A warp writes one group of 16 tokens of one head (18 d bytes side by side) from wherever its tokens were.  Block = (sequence,
-// two groups), the warps take (head, group) in turn.  A block is over after two dependent round trips (who
-// moves, the move), and eight of them share an SM; the groups ahead of the first hole have nothing to do.
-constexpr int MOVE_THREADS = 256, MOVE_GROUPS = 2;
+// A warp writes one group of 16 tokens of one head (18 d bytes side by side) from wherever its tokens were.  Every block has an equal
+// run of the groups to move, whatever the sequences are; the warps take the heads, and while a group moves the
+// places of the next one's tokens are fetched.
+constexpr int MOVE_THREADS = 256;
 template <int D>
-__global__ void __launch_bounds__(MOVE_THREADS) k_kv4_move(Kv4 c, const int32_t* __restrict__ table, PlanWs ws, int blocks) {
+__global__ void __launch_bounds__(MOVE_THREADS) k_kv4_move(Kv4 c, const int32_t* __restrict__ table, PlanWs ws) {
   constexpr int ROW16 = D / 32;            // 16-byte pieces of a code row
   constexpr int CODES = 2 * 16 * ROW16;    // of a group: keys, then values
-  const int i = blockIdx.x / blocks, base = (blockIdx.x % blocks) * (16 * MOVE_GROUPS), lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
-  // every lane: where row (lane % 16) of either group was, and the groups' pages; asked for at once, used if they are valid
-  const int ok = *ws.ok, cnt = ws.cnt[i], first = ws.info[i] * c.ps;
-  int src[MOVE_GROUPS], page[MOVE_GROUPS];
-#pragma unroll
-  for (int m = 0; m < MOVE_GROUPS; ++m) {
-    const int j = base + 16 * m + (lane & 15);
-    src[m] = j < ws.cap ? ws.src[(size_t)i * ws.cap + j] : 0;
-    page[m] = j < ws.cap ? table[(size_t)i * c.max_pages + j / c.ps] : 0;
+  const int total = ws.goff[c.n_seqs];
+  if (!*ws.ok || !total) return;
+  const int t0 = (int)((long long)total * blockIdx.x / gridDim.x), t1 = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
+  if (t0 >= t1) return;
+  int i = 0;
+  for (int hi = c.n_seqs; hi - i > 1;) {  // goff[i] <= t0 < goff[hi]
+    const int mid = (i + hi) >> 1;
+    if (ws.goff[mid] <= t0) i = mid;
+    else hi = mid;
   }
-  if (!ok || base + 16 * MOVE_GROUPS <= first || base >= cnt) return;
-  for (int task = threadIdx.x >> 5; task < MOVE_GROUPS * c.Hkv; task += MOVE_THREADS / 32) {
-    const int m = task / c.Hkv, h = task % c.Hkv, j0 = base + 16 * m;
-    if (j0 < first || j0 >= cnt) continue;
-    const int rows = min(16, cnt - j0);
-    const int from = (lane & 15) < rows ? (m ? src[1] : src[0]) : 0;
-    uint8_t* g = kv4_group(c, m ? page[1] : page[0], h, (j0 % c.ps) >> 4);
-    uint4 code[CODES / 32];
+  while (ws.goff[i + 1] <= t0) ++i;
+  // group t: rows of it, its page, and (lane r) where row r % 16 was
+  struct Group {
+    int rows, page, slot, src;
+  };
+  auto fetch = [&](int t) {
+    while (ws.goff[i + 1] <= t) ++i;
+    Group g;
+    const int j0 = ws.info[i] * c.ps + (t - ws.goff[i]) * 16;
+    g.rows = min(16, ws.cnt[i] - j0);
+    g.slot = j0 % c.ps;
+    g.page = table[(size_t)i * c.max_pages + j0 / c.ps];
+    g.src = (lane & 15) < g.rows ? ws.src[(size_t)i * ws.cap + j0 + (lane & 15)] : 0;
+    return g;
+  };
+  Group next = fetch(t0);
+  for (int t = t0; t < t1; ++t) {
+    const Group now = next;
+    if (t + 1 < t1) next = fetch(t + 1);
+    const int from = (lane & 15) < now.rows ? now.src : 0;
+    for (int h = warp; h < c.Hkv; h += MOVE_THREADS / 32) {
+      uint8_t* g = kv4_group(c, now.page, h, now.slot >> 4);
+      uint4 code[CODES / 32];
 #pragma unroll
-    for (int q = 0; q < CODES / 32; ++q) {
-      const int e = q * 32 + lane, which = e / (16 * ROW16), r = e / ROW16 % 16, x = e % ROW16;
-      const int s = __shfl_sync(0xffffffffu, from, r);
-      const uint8_t* a = kv4_group(c, s / c.ps, h, (s % c.ps) >> 4) + (which ? kv4_vc(D, s & 15) : kv4_kc(D, s & 15)) + 16 * x;
-      code[q] = r < rows ? *reinterpret_cast<const uint4*>(a) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    // scales: lane = (which, row), D / 16 bytes each
-    const int which = lane >> 4, r = lane & 15;
-    const uint8_t* a = kv4_group(c, from / c.ps, h, (from % c.ps) >> 4) + (which ? kv4_vs(D, from & 15) : kv4_ks(D, from & 15));
-    uint32_t scale[D / 64];
+      for (int q = 0; q < CODES / 32; ++q) {
+        const int e = q * 32 + lane, which = e / (16 * ROW16), r = e / ROW16 % 16, x = e % ROW16;
+        const int s = __shfl_sync(0xffffffffu, from, r);
+        const uint8_t* a = kv4_group(c, s / c.ps, h, (s % c.ps) >> 4) + (which ? kv4_vc(D, s & 15) : kv4_kc(D, s & 15)) + 16 * x;
+        code[q] = r < now.rows ? *reinterpret_cast<const uint4*>(a) : make_uint4(0u, 0u, 0u, 0u);
+      }
+      // scales: lane = (which, row), D / 16 bytes each
+      const int which = lane >> 4, r = lane & 15;
+      const uint8_t* a = kv4_group(c, from / c.ps, h, (from % c.ps) >> 4) + (which ? kv4_vs(D, from & 15) : kv4_ks(D, from & 15));
+      uint32_t scale[D / 64];
 #pragma unroll
-    for (int q = 0; q < D / 64; ++q) scale[q] = r < rows ? reinterpret_cast<const uint32_t*>(a)[q] : 0u;
+      for (int q = 0; q < D / 64; ++q) scale[q] = r < now.rows ? reinterpret_cast<const uint32_t*>(a)[q] : 0u;
 #pragma unroll
-    for (int q = 0; q < CODES / 32; ++q) {
-      const int e = q * 32 + lane, wh = e / (16 * ROW16), rr = e / ROW16 % 16, x = e % ROW16;
-      if (rr < rows) *reinterpret_cast<uint4*>(g + (wh ? kv4_vc(D, rr) : kv4_kc(D, rr)) + 16 * x) = code[q];
-    }
-    if (r < rows) {
-      uint32_t* b = reinterpret_cast<uint32_t*>(g + (which ? kv4_vs(D, r) : kv4_ks(D, r)));
+      for (int q = 0; q < CODES / 32; ++q) {
+        const int e = q * 32 + lane, wh = e / (16 * ROW16), rr = e / ROW16 % 16, x = e % ROW16;
+        if (rr < now.rows) *reinterpret_cast<uint4*>(g + (wh ? kv4_vc(D, rr) : kv4_kc(D, rr)) + 16 * x) = code[q];
+      }
+      if (r < now.rows) {
+        uint32_t* b = reinterpret_cast<uint32_t*>(g + (which ? kv4_vs(D, r) : kv4_ks(D, r)));
 #pragma unroll
-      for (int q = 0; q < D / 64; ++q) b[q] = scale[q];
+        for (int q = 0; q < D / 64; ++q) b[q] = scale[q];
+      }
     }
   }
 }
@@ -579,13 +616,14 @@ size_t compact_workspace(const Kv4& c, int keep_stride, uint8_t* base, PlanWs* w
   const long long most = (long long)c.n_seqs * ((cap + c.ps - 1) / c.ps);
   const int list = (int)(most < c.n_pages ? most : c.n_pages);
   const size_t row = kv4_align(4 * (size_t)c.n_seqs);
-  const size_t l = 256 + 3 * row, s = l + kv4_align(4 * (size_t)list);
+  const size_t l = 256 + 4 * row + 256, s = l + kv4_align(4 * (size_t)list);
   if (ws) {
     *ws = {};
     ws->ok = (int32_t*)base;
     ws->off = (int32_t*)(base + 256);
     ws->info = (int32_t*)(base + 256 + row);
     ws->cnt = (int32_t*)(base + 256 + 2 * row);
+    ws->goff = (int32_t*)(base + 256 + 3 * row);
     ws->list = (int32_t*)(base + l);
     ws->list_max = list;
     ws->src = (int32_t*)(base + s);
@@ -699,7 +737,7 @@ extern "C" int im_kv4_append(const im_kv4* cache, const im_kv4_map* from, const 
   if (e == cudaSuccess && n_tokens > 0) {
     const int x = (n_tokens * (c.d / 16) + STORE_THREADS - 1) / STORE_THREADS;
     const long long tasks = (long long)c.n_seqs * c.Hkv, copiers = tasks < 592 ? tasks : 592;  // (four blocks per SM)
-    const dim3 grid(x, 2 * c.Hkv + (int)((copiers + x - 1) / x));
+    const dim3 grid(x, c.Hkv + (int)((copiers + x - 1) / x));
     if (dtype == IM_BF16)
       e = kv4_launch(k_kv4_store<bf16>, grid, STORE_THREADS, 0, s, true, c, to->table, to->lens, (const bf16*)k, k_stride, (const bf16*)v,
                      v_stride, n_tokens, cu_new, ws);
@@ -764,16 +802,18 @@ extern "C" int im_kv4_compact(const im_kv4* cache, const im_kv4_map* from, const
   PlanWs ws;
   if (!workspace || ((uintptr_t)workspace & 255) || compact_workspace(c, keep_stride, (uint8_t*)workspace, &ws) > workspace_bytes)
     return kv4_fail(IM_ERR_CAPACITY, fn, "workspace missing, misaligned or too small");
-  const int blocks = (ws.cap + 16 * MOVE_GROUPS - 1) / (16 * MOVE_GROUPS);
-  if ((long long)blocks * c.n_seqs > 0x7fffffffll) return kv4_fail(IM_ERR_ARG, fn, "map too large");
+  // eight blocks per SM, and no more than there can be groups
+  const long long groups = (long long)((ws.cap + 15) / 16) * c.n_seqs;
+  const int sms = kv4_sm_count();
+  if (sms < 1) return kv4_fail(IM_ERR_CUDA, fn, "no usable CUDA device");
   cudaStream_t s = (cudaStream_t)cuda_stream;
   cudaError_t e = kv4_launch(k_kv4_scan, dim3(c.n_seqs), SCAN_THREADS, 0, s, false, c, *from, keep, keep_stride, ws);
   if (e == cudaSuccess) e = launch_plan(k_kv4_plan<PLAN_COMPACT>, c, s, true, c, *from, *to, (const int32_t*)nullptr, 0, ws);
   if (e == cudaSuccess) {
-    const dim3 grid((unsigned)(blocks * c.n_seqs));
-    if (c.d == 64) e = kv4_launch(k_kv4_move<64>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, blocks);
-    else if (c.d == 128) e = kv4_launch(k_kv4_move<128>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, blocks);
-    else e = kv4_launch(k_kv4_move<256>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws, blocks);
+    const dim3 grid((unsigned)(groups < 8 * sms ? groups : 8 * sms));
+    if (c.d == 64) e = kv4_launch(k_kv4_move<64>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws);
+    else if (c.d == 128) e = kv4_launch(k_kv4_move<128>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws);
+    else e = kv4_launch(k_kv4_move<256>, grid, MOVE_THREADS, 0, s, true, c, (const int32_t*)to->table, ws);
   }
   return launched(e);
 }

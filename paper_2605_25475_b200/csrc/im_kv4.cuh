@@ -91,5 +91,6 @@ inline cudaError_t kv4_launch(void (*kernel)(KArgs...), dim3 grid, int threads, 
 int kv4_describe(const im_kv4* cache, const char* fn, Kv4* out);
 int kv4_check_map(const im_kv4_map* m, const char* fn);
 int kv4_fail(int code, const char* fn, const char* what);
+int kv4_sm_count();  // of the current device (0: none)
 size_t kv4_attention_workspace(const Kv4& c, int max_q, int n_q_heads);
 inline size_t kv4_align(size_t b) { return (b + 255) & ~(size_t)255; }

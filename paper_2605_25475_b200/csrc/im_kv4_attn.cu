@@ -76,11 +76,12 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   int workers, per;
   const Deal deal = deal_line<ROWS, TILE, THREADS>(a, s_cum, s_scan, (long long)gridDim.x * WARPS, &workers, &per);
-  empty_rows<D>(a, out, lse);
   const int worker = warp * gridDim.x + blockIdx.x;  // neighbours in the line sit on different SMs
-  if (worker >= workers) return;
   const long long t0 = worker * deal.q + min((long long)worker, deal.rest), t1 = t0 + deal.q + (worker < deal.rest ? 1 : 0);
-  if (t0 >= t1) return;
+  if (worker >= workers || t0 >= t1) {
+    empty_rows<D>(a, out, lse, warp, WARPS);
+    return;
+  }
   long long off;
   const int i0 = find_tile<ROWS, TILE, THREADS>(a, s_cum, per, t0, &off);
   // ---- the copies' side: sequence pi, KV head ph, row block pr, tile p_tile
@@ -465,6 +466,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
     if (lane == 0) atomicOr(c.status, IM_KV4_TIMEOUT);
     for (int k = 0; k < 64; ++k) __nanosleep(1000);
   }
+  empty_rows<D>(a, out, lse, warp, WARPS);
 }
 
 // ------------------------------------------------------------------ host side

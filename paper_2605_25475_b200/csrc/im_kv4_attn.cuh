@@ -36,8 +36,6 @@ struct AttnArgs {
   AttnWs ws;
 };
 
-// number of SMs of the current device (0: none)
-int kv4_sm_count();
 // many query rows (head_dim 64 or 128): workspace (ws, if not null, is set up in `base`), launch
 size_t kv4_chunk_workspace(const Kv4& c, uint8_t* base, AttnWs* ws);
 cudaError_t kv4_launch_chunk(const AttnArgs& a, int dtype, int out_f32, const void* q, void* out, float* lse, int grid, cudaStream_t s);
@@ -176,20 +174,21 @@ __device__ __forceinline__ Deal deal_line(const AttnArgs& a, long long* s_cum, l
   }
   return d;
 }
-// rows of sequences that hold nothing: zeros, and no sum.  The sequences go round the CTAs.
+// Rows of sequences that hold nothing: zeros, and no sum.  The sequences go round the CTAs, here to one warp of this CTA's.
 template <int D, typename OutT>
-__device__ __forceinline__ void empty_rows(const AttnArgs& a, OutT* out, float* lse) {
-  for (int i = blockIdx.x; i < a.c.n_seqs; i += gridDim.x) {
+__device__ __forceinline__ void empty_rows(const AttnArgs& a, OutT* out, float* lse, int warp, int warps) {
+  const int lane = threadIdx.x & 31;
+  for (int i = blockIdx.x + warp * gridDim.x; i < a.c.n_seqs; i += gridDim.x * warps) {
     if (a.lens[i] > 0) continue;
     int first, nq;
     queries_of(a, i, &first, &nq);
     const size_t at = (size_t)first * a.H, n = (size_t)nq * a.H;
-    for (size_t x = threadIdx.x; x < n * (D / 8); x += blockDim.x) {
+    for (size_t x = lane; x < n * (D / 8); x += 32) {
       const float zero[8] = {};
       put8(out + at * D + 8 * x, zero);
     }
     if (lse)
-      for (size_t x = threadIdx.x; x < n; x += blockDim.x) lse[at + x] = NEG_INF;
+      for (size_t x = lane; x < n; x += 32) lse[at + x] = NEG_INF;
   }
 }
 // the sequence that tile t (< total) of the line lies in, and the tile's place in it

@@ -210,7 +210,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
   const uint32_t tmem = sh.tmem;
   const int worker = blockIdx.x;
   const long long t0 = worker * deal.q + min((long long)worker, deal.rest), t1 = t0 + deal.q + (worker < deal.rest ? 1 : 0);
-  empty_rows<D>(a, out, lse);
   bool ok = true;
   if (worker < workers && t0 < t1) {
     Walk w;
@@ -543,6 +542,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
       for (int k = 0; k < 64; ++k) __nanosleep(1000);
     }
   }
+  empty_rows<D>(a, out, lse, warp, THREADS / 32);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (warp == W_MMA) {
