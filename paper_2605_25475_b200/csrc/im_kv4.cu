@@ -14,7 +14,7 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int PLAN_CTAS = 8, PLAN_THREADS = 512, PLAN_WARPS = PLAN_THREADS / 32;
+constexpr int PLAN_CTAS = 8, PLAN_THREADS = 1024, PLAN_SEG = 128, PLAN_WARPS = PLAN_THREADS / 32;
 constexpr int SCAN_THREADS = 1024;
 constexpr int PLAN_ONE_CTA_PAGES = 8192;
 enum { PLAN_APPEND = 0, PLAN_COMPACT = 1 };
@@ -22,6 +22,7 @@ enum { PLAN_APPEND = 0, PLAN_COMPACT = 1 };
 // What a plan hands to the kernels behind it (in the caller's workspace; every word that is read is written by the same call).
 struct PlanWs {
   int32_t* ok;    // [1] 1: the call is made, 0: nothing changes
+  int32_t* len;   // [n_seqs] lengths before the call
   int32_t* off;   // [n_seqs] rank of the sequence's first new page
   int32_t* info;  // [n_seqs] append: the shared last page whose tokens are copied, or -1; compact: pages that stay
   int32_t* cnt;   // [n_seqs] compact: survivors, or -1 for a row that is out of order
@@ -86,9 +87,9 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
   bool bad = false, full = false;
   for (int base = 0; base < c.n_seqs; base += PLAN_THREADS) {
     const int i = base + tid;
-    int need = 0, move = 0, info = MODE == PLAN_APPEND ? -1 : 0;
+    int need = 0, move = 0, info = MODE == PLAN_APPEND ? -1 : 0, L = 0;
     if (i < c.n_seqs) {
-      const int L = from.lens[i];
+      L = from.lens[i];
       if (MODE == PLAN_APPEND) {
         const int add = new_tokens(cu, i, n_tokens, &bad);
         if (L < 0 || L > c.max_pages * c.ps) {
@@ -119,6 +120,7 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
     const long long before = block_scan<PLAN_WARPS>((long long)need, s_warp, &chunk);
     if (rank == 0 && i < c.n_seqs) {
       const long long o = total + before;
+      ws.len[i] = L;
       ws.off[i] = (int)(o < 0x7fffffff ? o : 0x7fffffff);
       if (MODE == PLAN_APPEND) ws.info[i] = info;
     }
@@ -146,16 +148,12 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
     if (lane == 0) s_free[warp] = n;
   }
   __syncthreads();
-  if (tid == 0) {
-    int n = 0;
-    if (want)
-      for (int w = 0; w < PLAN_WARPS; ++w) {
-        const int k = s_free[w];
-        s_free[w] = n;
-        n += k;
-      }
-    s_count = n;
+  if (warp == 0) {
+    const int k = want ? s_free[lane] : 0, incl = warp_scan_incl(k, lane);
+    s_free[lane] = incl - k;
+    if (lane == 31) s_count = incl;
   }
+  __syncthreads();
   cluster.sync();
   int first = 0, free_pages = 0;
   if (want)
@@ -186,9 +184,11 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
     }
   }
   cluster.sync();  // (also the last read of another CTA's shared memory)
-  // ---- rows
-  for (int i = rank * PLAN_WARPS + warp; i < c.n_seqs; i += ctas * PLAN_WARPS) {
-    const int L = from.lens[i];
+  // ---- rows, in pieces of PLAN_SEG entries
+  const int segs = (c.max_pages + PLAN_SEG - 1) / PLAN_SEG;
+  for (long long task = rank * PLAN_WARPS + warp; task < (long long)c.n_seqs * segs; task += ctas * PLAN_WARPS) {
+    const int i = (int)(task / segs), j0 = (int)(task % segs) * PLAN_SEG;
+    const int L = ws.len[i], off = ws.off[i], info = ws.info[i];
     const size_t row = (size_t)i * c.max_pages;
     const int held = L < 0 ? 0 : (int)min((long long)c.max_pages, ((long long)L + c.ps - 1) / c.ps);
     int kept = held, pages = held, len = L;
@@ -197,21 +197,27 @@ k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu
         bool b = false;
         len = L + new_tokens(cu, i, n_tokens, &b);
         pages = (len + c.ps - 1) / c.ps;
-        if (ws.info[i] >= 0) kept = held - 1;
+        if (info >= 0) kept = held - 1;
       } else {
         len = ws.cnt[i];
         pages = (len + c.ps - 1) / c.ps;
-        kept = ws.info[i];
+        kept = info;
       }
     }
-    const int off = ws.off[i];
-    for (int j = lane; j < max(held, pages); j += 32) {
-      const int old = j < held ? from.table[row + j] : -1;
-      if (ok && j >= kept && j < held && old >= 0 && old < c.n_pages) atomicSub(to.refs + old, 1);
-      if (j < pages) to.table[row + j] = j < kept ? old : ws.list[off + j - kept];
+    int old[PLAN_SEG / 32], now[PLAN_SEG / 32];
+#pragma unroll
+    for (int q = 0; q < PLAN_SEG / 32; ++q) {
+      const int j = j0 + 32 * q + lane;
+      old[q] = j < held ? from.table[row + j] : -1;
+      now[q] = j < kept || j >= pages ? old[q] : ws.list[off + j - kept];
     }
-    __syncwarp();
-    if (lane == 0) to.lens[i] = len;
+#pragma unroll
+    for (int q = 0; q < PLAN_SEG / 32; ++q) {
+      const int j = j0 + 32 * q + lane;
+      if (ok && j >= kept && j < held && old[q] >= 0 && old[q] < c.n_pages) atomicSub(to.refs + old[q], 1);
+      if (j < pages) to.table[row + j] = now[q];
+    }
+    if (j0 == 0 && lane == 0) to.lens[i] = len;
   }
 }
 
@@ -595,12 +601,13 @@ size_t append_workspace(const Kv4& c, long long n_tokens, uint8_t* base, PlanWs*
   // a sequence needs at most one page per page_size new tokens, one for the remainder and one of its own
   const long long most = n_tokens / c.ps + 2ll * c.n_seqs;
   const int list = (int)(most < c.n_pages ? most : c.n_pages);
-  const size_t a = 256, b = a + kv4_align(4 * (size_t)c.n_seqs), l = b + kv4_align(4 * (size_t)c.n_seqs);
+  const size_t row = kv4_align(4 * (size_t)c.n_seqs), l = 256 + 3 * row;
   if (ws) {
     *ws = {};
     ws->ok = (int32_t*)base;
-    ws->off = (int32_t*)(base + a);
-    ws->info = (int32_t*)(base + b);
+    ws->len = (int32_t*)(base + 256);
+    ws->off = (int32_t*)(base + 256 + row);
+    ws->info = (int32_t*)(base + 256 + 2 * row);
     ws->list = (int32_t*)(base + l);
     ws->list_max = list;
   }
@@ -616,14 +623,15 @@ size_t compact_workspace(const Kv4& c, int keep_stride, uint8_t* base, PlanWs* w
   const long long most = (long long)c.n_seqs * ((cap + c.ps - 1) / c.ps);
   const int list = (int)(most < c.n_pages ? most : c.n_pages);
   const size_t row = kv4_align(4 * (size_t)c.n_seqs);
-  const size_t l = 256 + 4 * row + 256, s = l + kv4_align(4 * (size_t)list);
+  const size_t l = 256 + 5 * row + 256, s = l + kv4_align(4 * (size_t)list);
   if (ws) {
     *ws = {};
     ws->ok = (int32_t*)base;
     ws->off = (int32_t*)(base + 256);
     ws->info = (int32_t*)(base + 256 + row);
     ws->cnt = (int32_t*)(base + 256 + 2 * row);
-    ws->goff = (int32_t*)(base + 256 + 3 * row);
+    ws->len = (int32_t*)(base + 256 + 3 * row);
+    ws->goff = (int32_t*)(base + 256 + 4 * row);
     ws->list = (int32_t*)(base + l);
     ws->list_max = list;
     ws->src = (int32_t*)(base + s);
