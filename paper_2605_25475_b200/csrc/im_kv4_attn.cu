@@ -506,8 +506,10 @@ cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* 
 
 // query rows of a KV head in the longest sequence
 long long rows_of(const Kv4& c, bool ragged, int max_q, int n_q_heads) { return (long long)(ragged ? (max_q > 0 ? max_q : 1) : 1) * (n_q_heads / c.Hkv); }
-// Which kernel.  Beyond 16 rows (two column tiles) the streaming kernel would unpack the cache again for every 16.
-bool by_chunks(const Kv4& c, long long rows) { return rows > 16 && c.d != 256; }
+// Which kernel.  The streaming kernel unpacks the cache again for every 16 rows (two column tiles), the other one once for up to
+// 256, at a higher price per tile.  8 sequences of 12000 entries, 8 KV heads of 128, streaming / other: 24 rows 85 / 106 us,
+// 36 rows 117 / 107; 4 heads of 64: 24 rows 36 / 46, 36 rows 43 / 46, 52 rows 51 / 47.
+bool by_chunks(const Kv4& c, long long rows) { return rows > 32 && c.d != 256; }
 
 }  // namespace
 

@@ -283,21 +283,33 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
           const bool whole = __all_sync(0xffffffffu, seen >= KT && none == 0);
           if (ut == 0) sh.hidden[s] = none;
           // (every offset below is a constant but for those of the lane)
+          // The loads of a batch stand ahead of its stores, which the compiler could not know to be elsewhere.
           auto unpack = [&](auto all) {
+            constexpr int ROUNDS = KT / STEP, BATCH = 8;  // words of a thread: 2 ROUNDS, keys then values
 #pragma unroll
-            for (int v = 0; v < 2; ++v)
+            for (int y0 = 0; y0 < 2 * ROUNDS; y0 += BATCH) {
+              uint32_t code[BATCH], by[BATCH];
 #pragma unroll
-              for (int p = 0; p < KT / STEP; ++p) {
+              for (int y = 0; y < BATCH; ++y) {
+                const int v = (y0 + y) / ROUNDS, p = (y0 + y) % ROUNDS;
                 const int group = p * STEP / 16, up = p * STEP % 16;  // row r0 + p STEP = row r0 + up of the group
-                const uint32_t code = *reinterpret_cast<const uint32_t*>(codes + group * Z::GROUP + v * 9 * D + up * (D / 2));
-                uint32_t sc = scales[group * Z::GROUP + v * 9 * D + up * (D / 16)];
-                if (!decltype(all)::value && (r0 + p * STEP >= seen || ((none >> group) & 1))) sc = 0;
-                sc = kv4_f16x2_e4m3(sc);
-                const uint32_t by = __byte_perm(sc, sc, 0x1010);
-                uint32_t x[4];
-                kv4_f16_e2m1(code, x);
-                *reinterpret_cast<uint4*>(dst + v * Z::KV + p * STEP * 128) = make_uint4(mul2(x[0], by), mul2(x[1], by), mul2(x[2], by), mul2(x[3], by));
+                code[y] = *reinterpret_cast<const uint32_t*>(codes + group * Z::GROUP + v * 9 * D + up * (D / 2));
+                by[y] = scales[group * Z::GROUP + v * 9 * D + up * (D / 16)];
+                if (!decltype(all)::value && (r0 + p * STEP >= seen || ((none >> group) & 1))) by[y] = 0;
               }
+#pragma unroll
+              for (int y = 0; y < BATCH; ++y) {
+                by[y] = kv4_f16x2_e4m3(by[y]);
+                by[y] = __byte_perm(by[y], by[y], 0x1010);
+              }
+#pragma unroll
+              for (int y = 0; y < BATCH; ++y) {
+                const int v = (y0 + y) / ROUNDS, p = (y0 + y) % ROUNDS;
+                uint32_t x[4];
+                kv4_f16_e2m1(code[y], x);
+                *reinterpret_cast<uint4*>(dst + v * Z::KV + p * STEP * 128) = make_uint4(mul2(x[0], by[y]), mul2(x[1], by[y]), mul2(x[2], by[y]), mul2(x[3], by[y]));
+              }
+            }
           };
           if (whole) unpack(std::true_type{});
           else unpack(std::false_type{});
@@ -378,37 +390,36 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
         int ex = 0;
         {  // the row of Q (the products that read the last one are complete: their scores have been waited for)
           const uint4* src = reinterpret_cast<const uint4*>(q + (size_t)(g.first + token) * a.q_stride + (size_t)head * D);
-          float by = 1.f;
+          uint4 v[D / 8];
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) v[k] = there ? src[k] : make_uint4(0u, 0u, 0u, 0u);
           if constexpr (std::is_same<T, bf16>::value) {
             float amax = 0.f;
-            if (there)
-#pragma unroll 4
-              for (int k = 0; k < D / 8; ++k) {
-                const uint4 v = src[k];
-                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                  const float2 y = two_of((const bf16*)nullptr, u[b]);
-                  amax = fmaxf(amax, fmaxf(fabsf(y.x), fabsf(y.y)));
-                }
+            for (int k = 0; k < D / 8; ++k) {
+              const uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+              for (int b = 0; b < 4; ++b) {
+                const float2 y = two_of((const bf16*)nullptr, u[b]);
+                amax = max3(amax, fabsf(y.x), fabsf(y.y));
               }
+            }
             ex = row_exponent(amax);
-            by = exp2i(ex);
-          }
-#pragma unroll 4
-          for (int k = 0; k < D / 8; ++k) {
-            uint4 v = there ? src[k] : make_uint4(0u, 0u, 0u, 0u);
-            if constexpr (std::is_same<T, bf16>::value) {
-              uint32_t u[4] = {v.x, v.y, v.z, v.w};
+            const float by = exp2i(ex);
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k) {
+              uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
               for (int b = 0; b < 4; ++b) {
                 const float2 y = two_of((const bf16*)nullptr, u[b]);
                 u[b] = pack_f16(y.x * by, y.y * by);
               }
-              v = make_uint4(u[0], u[1], u[2], u[3]);
+              v[k] = make_uint4(u[0], u[1], u[2], u[3]);
             }
-            *reinterpret_cast<uint4*>(s_q + x * Z::Q + (k >> 3) * (ROWS * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((k & 7) ^ (r & 7)) << 4)) = v;
           }
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k)
+            *reinterpret_cast<uint4*>(s_q + x * Z::Q + (k >> 3) * (ROWS * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((k & 7) ^ (r & 7)) << 4)) = v[k];
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           mbar_arrive(smem_u32(&sh.qfull[x]));
         }
