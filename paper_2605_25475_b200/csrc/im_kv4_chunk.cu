@@ -37,7 +37,7 @@ struct Sizes {
 };
 
 struct Shared {
-  unsigned long long raw_full[RAW], raw_empty[RAW], full[STAGES], empty[STAGES], qfull[QT], sfull[QT], sempty[QT], pfull[QT], pvdone[QT], odone[QT], ofree[QT];
+  unsigned long long raw_full[RAW], raw_empty[RAW], full[STAGES], empty[STAGES], qfull[QT], sfull[QT], sempty[QT], pfull[QT][2], pvdone[QT], odone[QT], ofree[QT];
   long long cum[THREADS + 1], scan[THREADS / 32];
   int no_page[RAW];   // groups of a raw tile that have no page (bits)
   int hidden[STAGES]; // the same for the unpacked tile
@@ -190,7 +190,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
       mbar_init(smem_u32(&sh.qfull[g]), ROWS);
       mbar_init(smem_u32(&sh.sfull[g]), 1);
       mbar_init(smem_u32(&sh.sempty[g]), ROWS);
-      mbar_init(smem_u32(&sh.pfull[g]), ROWS);
+      mbar_init(smem_u32(&sh.pfull[g][0]), ROWS);
+      mbar_init(smem_u32(&sh.pfull[g][1]), ROWS);
       mbar_init(smem_u32(&sh.pvdone[g]), 1);
       mbar_init(smem_u32(&sh.odone[g]), 1);
       mbar_init(smem_u32(&sh.ofree[g]), ROWS);
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
         ok = scores(n, cnt, true);
         for (int j = 0; j < nt && ok; ++j, ++n, ++cnt) {
           if (j + 1 < nt && !scores(n + 1, cnt + 1, false)) { ok = false; break; }
-          if (!mbar_wait(smem_u32(&sh.pfull[x]), (uint32_t)(cnt & 1), abort_flag)) { ok = false; break; }
+          if (!mbar_wait(smem_u32(&sh.pfull[x][cnt & 1]), (uint32_t)((cnt >> 1) & 1), abort_flag)) { ok = false; break; }
           if (j == 0 && segs > 0 && !mbar_wait(smem_u32(&sh.ofree[x]), (uint32_t)((segs - 1) & 1), abort_flag)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t va = kv + (n % STAGES) * Z::STAGE + Z::KV;
@@ -508,7 +509,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
           if (!ok) break;
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          mbar_arrive(smem_u32(&sh.pfull[x]));
+          mbar_arrive(smem_u32(&sh.pfull[x][k & 1]));  // (a barrier per parity: a warp may be a tile ahead of the others)
         }
         if (!ok) break;
         cnt += nt;

@@ -353,6 +353,31 @@ def test_attention_of_a_chunk(im, d):
     pair.attend([130, 129, 0, 64], 14, BF, True, causal=False)
 
 
+@pytest.mark.parametrize("d,dtype", [(128, BF), (128, HF), (64, BF)])
+def test_many_rows_agree_with_few_rows_over_a_long_cache(im, d, dtype):
+    """The kernel for many query rows against the one for few (max_q chooses it) on 520 tokens x 9000 entries, the reference
+    maximum rising all along (keys grow with their position), in fresh memory that holds NaN where nothing was written."""
+    n, nq, H, Hkv = 9000, 520, 8, 2
+    g = im.KV4Cache(1, -(-n // 64), -(-n // 64), Hkv, d, 64)
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    k, v = (torch.randn(n, Hkv, d, generator=gen, device="cuda:0") for _ in range(2))
+    k *= torch.linspace(0.2, 3.0, n, device="cuda:0")[:, None, None]
+    cu = ints([0, n])
+    g.append(k.to(BF), v.to(BF), cu)
+    q = torch.randn(nq, H, d, generator=gen, device="cuda:0").to(dtype)
+    cu = ints([0, nq])
+    want, wl = g.attend(q, cu, 1, out_f32=True, return_lse=True)
+    bound = torch.finfo(dtype).eps / 2 + 2.0 ** -11                                      # of the outputs and of p (for bf16), as above
+    for _ in range(4):
+        junk = torch.full((1 << 26,), float("nan"), device="cuda:0")
+        del junk
+        out, lse = g.attend(q, cu, nq, return_lse=True)
+        # p >= 0 sums to one over 9000 values of size one: sum p |v| is at most a few units
+        assert (out.float() - want).abs().max() <= bound * want.abs().max() + 2.0 ** -11 * v.abs().max()
+        assert (lse - wl).abs().max() <= 1e-4 * wl.abs().max()
+    assert g.status() == 0
+
+
 @pytest.mark.parametrize("spread", [1e-30, 30.0, 1e4])
 def test_attention_of_extreme_queries(im, spread):
     """Queries far outside f16's range, and scores that pick one entry alone."""
