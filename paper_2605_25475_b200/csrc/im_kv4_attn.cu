@@ -86,7 +86,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
   const int i0 = find_tile<ROWS, TILE, THREADS>(a, s_cum, per, t0, &off);
   // ---- the copies' side: sequence pi, KV head ph, row block pr, tile p_tile
   const Seq first = seq_of<ROWS, TILE>(a, i0);
-  const int item0 = (int)(off / first.tiles), tile0 = (int)(off % first.tiles);
+  const int item0 = (off >> 31) == 0 ? (int)((unsigned)off / (unsigned)first.tiles) : (int)(off / first.tiles), tile0 = (int)(off - (long long)item0 * first.tiles);
   Seq sq = first;
   int pi = i0, ph = item0 / first.rb, pr = item0 % first.rb, p_tile = tile0;
   int left = (int)(t1 - t0);           // tiles still to be requested
@@ -481,7 +481,7 @@ size_t workspace(const Kv4& c, long long rows, int nt, uint8_t* base, AttnWs* ws
 }
 
 template <int D, int NT, bool TWO, typename T, typename OutT>
-cudaError_t launch(const AttnArgs& a, const void* q, void* out, float* lse, int grid, cudaStream_t s) {
+cudaError_t launch(const AttnArgs& a, const void* q, void* out, float* lse, int grid, int rows, cudaStream_t s) {
   static bool flags[64] = {};
   bool* done = im_device_flag(flags);
   constexpr int smem = stages_of(D, NT) * warps_of(D, NT) * 2 * kv4_group_bytes(D);
@@ -493,15 +493,15 @@ cudaError_t launch(const AttnArgs& a, const void* q, void* out, float* lse, int 
   }
   cudaError_t e = kv4_launch(k_kv4_stream<D, NT, TWO, T, OutT>, dim3(grid), warps_of(D, NT) * 32, smem, s, false, a, (const T*)q, (OutT*)out, lse);
   if (e == cudaSuccess)
-    e = kv4_launch(k_kv4_join_tokens<D, 8 * NT, TILE, 4, OutT>, dim3(a.n_tokens, a.H), 4 * 32, 0, s, true, a, (OutT*)out, lse);
+    e = kv4_launch(k_kv4_join_seqs<D, 8 * NT, TILE, 4, OutT>, dim3(a.c.n_seqs, a.c.Hkv, rows < 32 ? (rows + 1) / 2 : 16), JOIN_WARPS * 32, 0, s, true, a, (OutT*)out, lse);
   return e;
 }
 
 template <int D, int NT>
-cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* q, void* out, float* lse, int grid, cudaStream_t s) {
+cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* q, void* out, float* lse, int grid, int rows, cudaStream_t s) {
   if (dtype == IM_BF16)
-    return out_f32 ? launch<D, NT, true, bf16, float>(a, q, out, lse, grid, s) : launch<D, NT, false, bf16, bf16>(a, q, out, lse, grid, s);
-  return out_f32 ? launch<D, NT, true, __half, float>(a, q, out, lse, grid, s) : launch<D, NT, true, __half, __half>(a, q, out, lse, grid, s);
+    return out_f32 ? launch<D, NT, true, bf16, float>(a, q, out, lse, grid, rows, s) : launch<D, NT, false, bf16, bf16>(a, q, out, lse, grid, rows, s);
+  return out_f32 ? launch<D, NT, true, __half, float>(a, q, out, lse, grid, rows, s) : launch<D, NT, true, __half, __half>(a, q, out, lse, grid, rows, s);
 }
 
 // query rows of a KV head in the longest sequence
@@ -561,11 +561,11 @@ extern "C" int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int 
     const cudaError_t e = kv4_launch_chunk(a, dtype, out_f32, q, out, lse, grid, s);
     return e == cudaSuccess ? IM_OK : im_fail_message(IM_ERR_CUDA, cudaGetErrorString(e));
   }
-  const int nt = rows <= 8 ? 1 : 2;
+  const int nt = rows <= 8 ? 1 : 2, few = rows < 32 ? (int)rows : 32;
   workspace(c, rows, nt, (uint8_t*)workspace_, &a.ws);
   auto go = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    return nt == 1 ? launch_types<D, 1>(a, dtype, out_f32, q, out, lse, grid, s) : launch_types<D, 2>(a, dtype, out_f32, q, out, lse, grid, s);
+    return nt == 1 ? launch_types<D, 1>(a, dtype, out_f32, q, out, lse, grid, few, s) : launch_types<D, 2>(a, dtype, out_f32, q, out, lse, grid, few, s);
   };
   const cudaError_t e = c.d == 64    ? go(std::integral_constant<int, 64>{})
                         : c.d == 128 ? go(std::integral_constant<int, 128>{})

@@ -162,7 +162,15 @@ __device__ __forceinline__ Deal deal_line(const AttnArgs& a, long long* s_cum, l
   const long long total = s_cum[THREADS];
   *workers = (int)min(most, max(1ll, total));
   *per_ = per;
-  const Deal d = {total / *workers, total % *workers, *workers};
+  Deal d;
+  d.workers = *workers;
+  if ((total >> 31) == 0) {  // (a 64-bit division costs 0.1 us)
+    d.q = (unsigned)total / (unsigned)*workers;
+    d.rest = (unsigned)total % (unsigned)*workers;
+  } else {
+    d.q = total / *workers;
+    d.rest = total % *workers;
+  }
   if (blockIdx.x == 0) {
     if (tid == 0) *a.ws.deal = d;
     long long at = s_cum[tid];
@@ -202,12 +210,13 @@ __device__ __forceinline__ int find_tile(const AttnArgs& a, const long long* s_c
   }
   int i = lo * per;
   *off = t - s_cum[lo];
-  while (true) {
+  while (per > 1) {
     const long long w = work_of(a, seq_of<ROWS, TILE>(a, i));
     if (*off < w) return i;
     *off -= w;
     ++i;
   }
+  return i;
 }
 
 // ---- joining the partial results of an item that workers w0 .. w1 share
@@ -220,56 +229,59 @@ __device__ __forceinline__ int worker_of(const Deal& d, long long x) {  // (of t
   }
   return (int)(x < big ? x / (d.q + 1) : d.rest + (x - big) / d.q);
 }
-// Row r of the item, by PER warps of the block (they share its results, so that all of them are asked for at once); `at`: the
-// row of out and lse.  The whole block calls it with the same w0, w1 where PER > 1.
+// Row r of the item, by PER warps of the block, which take its results in turn; `at`: the row of out and lse.  The whole block calls it
+// with the same w0, w1 where PER > 1.  Sums and vectors of a round are asked for together: one round trip for up to 8 PER results.
 template <int D, int ROWS, int PER, typename OutT>
 __device__ __forceinline__ void join_row(const AttnArgs& a, int w0, int w1, int r, bool there, int h, size_t at, OutT* out, float* lse) {
-  constexpr int CH = D / 32;
+  constexpr int CH = D / 32, ROUND = CH == 8 ? 4 : 8;
   __shared__ float s_acc[JOIN_WARPS][D], s_m[JOIN_WARPS], s_l[JOIN_WARPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % PER;
   float acc[CH], total = 0.f, m = NO_MAX;
 #pragma unroll
   for (int k = 0; k < CH; ++k) acc[k] = 0.f;
   if (there) {
-    // worker x's result: its run began ahead of the item, but for the first one's
+    // worker w's result: its run began ahead of the item, but for the first one's
     const float* part = a.ws.part + (size_t)r * (D + 4);
-    for (int b = w0 + sub * 32; b <= w1; b += PER * 32) {
-      const int mine = b + lane;
-      float2 ml = make_float2(NO_MAX, 0.f);
-      if (mine <= w1) ml = *reinterpret_cast<const float2*>(part + (size_t)(2 * mine + (mine == w0 ? 1 : 0)) * (ROWS * (D + 4)) + D);
-      float mb = ml.x;
+    auto result = [&](int w) { return part + (size_t)(2 * w + (w == w0 ? 1 : 0)) * (ROWS * (D + 4)); };
+    for (int b = w0 + sub; b <= w1; b += PER * ROUND) {
+      float v[ROUND][CH];
+      float2 ml[ROUND];
 #pragma unroll
-      for (int x = 1; x < 32; x <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, x));
-      mb = fmaxf(mb, m);
-      const float corr = ex2(m - mb), e = ex2(ml.x - mb);
-      m = mb;
-      float le = ml.y * e;
-#pragma unroll
-      for (int x = 1; x < 32; x <<= 1) le += __shfl_xor_sync(0xffffffffu, le, x);
-      total = fmaf(total, corr, le);
-#pragma unroll
-      for (int k = 0; k < CH; ++k) acc[k] *= corr;
-      const int n = min(32, w1 + 1 - b);
-#pragma unroll 8
-      for (int x = 0; x < n; ++x) {
-        const int y = b + x;
-        const float by = __shfl_sync(0xffffffffu, e, x);
-        const float* q = part + (size_t)(2 * y + (y == w0 ? 1 : 0)) * (ROWS * (D + 4));
+      for (int x = 0; x < ROUND; ++x) {
+        const int w = b + x * PER;
+        const float* q = result(min(w, w1));
+        ml[x] = *reinterpret_cast<const float2*>(q + D);
+        if (w > w1) ml[x] = make_float2(NO_MAX, 0.f);
         if constexpr (CH == 2) {
-          const float2 v = *reinterpret_cast<const float2*>(q + 2 * lane);
-          acc[0] = fmaf(v.x, by, acc[0]), acc[1] = fmaf(v.y, by, acc[1]);
+          const float2 y = *reinterpret_cast<const float2*>(q + 2 * lane);
+          v[x][0] = y.x, v[x][1] = y.y;
         } else {
 #pragma unroll
           for (int k = 0; k < CH; k += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(q + CH * lane + k);
-            acc[k] = fmaf(v.x, by, acc[k]), acc[k + 1] = fmaf(v.y, by, acc[k + 1]);
-            acc[k + 2] = fmaf(v.z, by, acc[k + 2]), acc[k + 3] = fmaf(v.w, by, acc[k + 3]);
+            const float4 y = *reinterpret_cast<const float4*>(q + CH * lane + k);
+            v[x][k] = y.x, v[x][k + 1] = y.y, v[x][k + 2] = y.z, v[x][k + 3] = y.w;
           }
         }
       }
+      float top = m;
+#pragma unroll
+      for (int x = 0; x < ROUND; ++x) top = fmaxf(top, ml[x].x);
+      const float corr = ex2(m - top);
+      m = top;
+      total *= corr;
+#pragma unroll
+      for (int k = 0; k < CH; ++k) acc[k] *= corr;
+#pragma unroll
+      for (int x = 0; x < ROUND; ++x) {
+        if (b + x * PER > w1) continue;
+        const float by = ex2(ml[x].x - top);
+        total = fmaf(ml[x].y, by, total);
+#pragma unroll
+        for (int k = 0; k < CH; ++k) acc[k] = fmaf(v[x][k], by, acc[k]);
+      }
     }
   }
-  if (PER > 1 && w1 - w0 >= 32) {  // (the same for the whole block)
+  if (PER > 1) {
 #pragma unroll
     for (int k = 0; k < CH; ++k) s_acc[warp][CH * lane + k] = acc[k];
     if (lane == 0) s_m[warp] = m, s_l[warp] = total;
@@ -300,21 +312,23 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, int w0, int w1, int 
   if (lse && lane == 0) lse[at] = total == 0.f ? NEG_INF : (m + log2f(total)) * LN2;
 }
 
-// Few rows: block = (query token, heads), PER warps per query head.  A row that sees nothing is written where it was found.
+// Few rows: block = (sequence, KV head, rows by z), PER warps per row.  A row that sees nothing is written where it was found.
 template <int D, int ROWS, int TILE, int PER, typename OutT>
-__global__ void __launch_bounds__(PER * 32) k_kv4_join_tokens(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
-  const int t = blockIdx.x, head = blockIdx.y, h = head / a.G;
-  const int i = kv4_find(a.cu, a.c.n_seqs, t);
-  if (i < 0) return;
+__global__ void __launch_bounds__(JOIN_WARPS * 32) k_kv4_join_seqs(const AttnArgs a, OutT* __restrict__ out, float* __restrict__ lse) {
+  const int i = blockIdx.x, h = blockIdx.y;
   const Seq s = seq_of<ROWS, TILE>(a, i);
-  const int r = (t - s.first) * a.G + head % a.G;
   pdl_wait();
   const Deal deal = *a.ws.deal;
+  const long long cum = a.ws.cum[i];
   if (!s.tiles) return;
-  const long long base = a.ws.cum[i] + ((long long)h * s.rb + r / ROWS) * s.tiles;
-  const int w0 = worker_of(deal, base), w1 = worker_of(deal, base + s.tiles - 1);
-  if (w0 == w1) return;  // written where it was computed
-  join_row<D, ROWS, PER>(a, w0, w1, r % ROWS, true, h, (size_t)t * a.H + head, out, lse);
+  for (int r0 = blockIdx.z * (JOIN_WARPS / PER); r0 < s.nq * a.G; r0 += gridDim.z * (JOIN_WARPS / PER)) {  // (rows of a block lie in one item)
+    const int r = r0 + (threadIdx.x >> 5) / PER;
+    const long long base = cum + ((long long)h * s.rb + r0 / ROWS) * s.tiles;
+    const int w0 = worker_of(deal, base), w1 = worker_of(deal, base + s.tiles - 1);
+    if (w0 == w1) continue;  // written where it was computed
+    join_row<D, ROWS, PER>(a, w0, w1, r % ROWS, r < s.nq * a.G, h, (size_t)(s.first + r / a.G) * a.H + h * a.G + r % a.G, out, lse);
+    __syncthreads();  // (its shared memory is used again)
+  }
 }
 // Many rows: block (w, y) = the item that worker w + 1's run begins inside, if w + 1 is the second worker on it (each shared item
 // has one); a warp per row, JOIN_WARPS rows by y.
