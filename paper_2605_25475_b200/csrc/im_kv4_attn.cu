@@ -138,6 +138,25 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
       }
     }
   };
+  // row 8 nt + g of Q, channels in the order the keys' lanes take them (the first segment's are asked for ahead of the tiles: a
+  // round trip less before the first product)
+  uint32_t raw[NT][D / 8];
+  auto load_q = [&](const Seq& sq_, int item_) {
+    const int h = item_ / sq_.rb, row0 = (item_ % sq_.rb) * ROWS, rows = min(ROWS, sq_.nq * a.G - row0);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = row0 + 8 * nt + g;
+      const bool there = 8 * nt + g < rows;
+      const T* src = q + (size_t)(sq_.first + (there ? r / a.G : 0)) * a.q_stride + (size_t)(h * a.G + (there ? r % a.G : 0)) * D;
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b) {  // 8 channels each
+        const int at = D == 64 ? 16 * cq + 8 * b : 128 * (b / 4) + 32 * cq + 8 * (b % 4);
+        const uint4 v = there ? *reinterpret_cast<const uint4*>(src + at) : make_uint4(0u, 0u, 0u, 0u);
+        raw[nt][4 * b] = v.x, raw[nt][4 * b + 1] = v.y, raw[nt][4 * b + 2] = v.z, raw[nt][4 * b + 3] = v.w;
+      }
+    }
+  };
+  load_q(first, item0);
 #pragma unroll 1
   for (int s = 0; s < STAGES && left > 0; ++s) request(s);
 
@@ -157,23 +176,12 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
     int lim_min = cs.L;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      // row 8 nt + g: channels in the order the keys' lanes take them
-      const int r = row0 + 8 * nt + g;
-      const bool there = 8 * nt + g < rows;
-      const T* src = q + (size_t)(cs.first + (there ? r / a.G : 0)) * a.q_stride + (size_t)(h * a.G + (there ? r % a.G : 0)) * D;
       float amax = 0.f;
-      uint32_t raw[D / 8];
-#pragma unroll
-      for (int b = 0; b < D / 32; ++b) {  // 8 channels each
-        const int at = D == 64 ? 16 * cq + 8 * b : 128 * (b / 4) + 32 * cq + 8 * (b % 4);
-        const uint4 v = there ? *reinterpret_cast<const uint4*>(src + at) : make_uint4(0u, 0u, 0u, 0u);
-        raw[4 * b] = v.x, raw[4 * b + 1] = v.y, raw[4 * b + 2] = v.z, raw[4 * b + 3] = v.w;
-      }
       int ex = 0;
       if constexpr (std::is_same<T, bf16>::value) {
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) {
-          const float2 x = two_of(src, raw[k]);
+          const float2 x = two_of((const bf16*)nullptr, raw[nt][k]);
           amax = fmaxf(amax, fmaxf(fabsf(x.x), fabsf(x.y)));
         }
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
@@ -182,14 +190,14 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
         const float by = exp2i(ex);
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) {
-          const float2 x = two_of(src, raw[k]);
-          raw[k] = pack_f16(x.x * by, x.y * by);
+          const float2 x = two_of((const bf16*)nullptr, raw[nt][k]);
+          raw[nt][k] = pack_f16(x.x * by, x.y * by);
         }
       }
 #pragma unroll
       for (int k = 0; k < KSTEPS; ++k) {
-        qf[nt][k][0] = raw[2 * k];
-        qf[nt][k][1] = raw[2 * k + 1];
+        qf[nt][k][0] = raw[nt][2 * k];
+        qf[nt][k][1] = raw[nt][2 * k + 1];
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {  // columns 2 cq + k of the scores
@@ -459,6 +467,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
         do cs = seq_of<ROWS, TILE>(a, ++ci);
         while (cs.tiles == 0);
       }
+      load_q(cs, item);
     }
   }
   if (!fine) {
