@@ -213,6 +213,10 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
     }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) lim_min = min(lim_min, __shfl_xor_sync(0xffffffffu, lim_min, o));
+    constexpr int FLUSH_TILES = std::is_same<OutT, float>::value ? FLUSH_STEPS / (TWO ? 4 : 2) : 1 << 30;
+    float* const place = a.ws.part + (size_t)(2 * worker + (t0 <= base ? 1 : 0)) * ROWS * (D + 4);  // of the segment's partial result
+    int fresh = 0, flushed = 0;  // tiles since the accumulators were emptied; how often they were
+    float fref[NT][2];           // reference maximum of what lies there
     float o[MT][NT][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -221,7 +225,38 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[m][nt][k] = 0.f;
 
+    // what lies in the segment's place, brought to the present reference maximum and added to the accumulators
+    auto add_flushed = [&](auto store) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int col = 8 * nt + 2 * cq + k;
+          if (col >= rows) continue;
+          float* p = place + (size_t)col * (D + 4) + g * (D / 8);
+          const float by = flushed ? ex2(fref[nt][k] - mref[nt][k]) : 0.f;
+#pragma unroll
+          for (int m = 0; m < MT; m += 2) {
+            if (flushed) {
+              const float4 y = *reinterpret_cast<const float4*>(p + 2 * m);
+              o[m][nt][k] = fmaf(y.x, by, o[m][nt][k]), o[m][nt][k + 2] = fmaf(y.y, by, o[m][nt][k + 2]);
+              o[m + 1][nt][k] = fmaf(y.z, by, o[m + 1][nt][k]), o[m + 1][nt][k + 2] = fmaf(y.w, by, o[m + 1][nt][k + 2]);
+            }
+            if constexpr (decltype(store)::value) {
+              *reinterpret_cast<float4*>(p + 2 * m) = make_float4(o[m][nt][k], o[m][nt][k + 2], o[m + 1][nt][k], o[m + 1][nt][k + 2]);
+              o[m][nt][k] = o[m][nt][k + 2] = o[m + 1][nt][k] = o[m + 1][nt][k + 2] = 0.f;
+            }
+          }
+          fref[nt][k] = mref[nt][k];
+        }
+    };
     for (; tile < end; ++tile) {
+      if (FLUSH_TILES < (1 << 30) && fresh == FLUSH_TILES) {
+        add_flushed(std::true_type{});
+        fresh = 0;
+        ++flushed;
+      }
+      ++fresh;
       if (!mbar_wait(bar0 + 8 * stage, parity)) {
         fine = false;
         break;
@@ -425,6 +460,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
     }
     if (!fine) break;
     // ---- the segment's result
+    if (FLUSH_TILES < (1 << 30) && flushed) add_flushed(std::false_type{});
     const bool complete = base >= t0 && end == cs.tiles;  // the item begins and ends here
     const float vup = kv4_pow2(kv4_exp(c.v_exp, h));
 #pragma unroll
@@ -452,7 +488,7 @@ k_kv4_stream(const AttnArgs a, const T* __restrict__ q, OutT* __restrict__ out, 
           }
           if (lse && g == 0) lse[at] = l[nt][k] == 0.f ? NEG_INF : (mref[nt][k] + log2f(l[nt][k])) * LN2;
         } else {
-          float* dst = a.ws.part + ((size_t)(2 * worker + (t0 <= base ? 1 : 0)) * ROWS + col) * (D + 4);
+          float* dst = place + (size_t)col * (D + 4);
 #pragma unroll
           for (int m = 0; m < MT; m += 2)
             *reinterpret_cast<float4*>(dst + g * (D / 8) + 2 * m) = make_float4(o[m][nt][k], o[m][nt][k + 2], o[m + 1][nt][k], o[m + 1][nt][k + 2]);
@@ -516,9 +552,10 @@ cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* 
 // query rows of a KV head in the longest sequence
 long long rows_of(const Kv4& c, bool ragged, int max_q, int n_q_heads) { return (long long)(ragged ? (max_q > 0 ? max_q : 1) : 1) * (n_q_heads / c.Hkv); }
 // Which kernel.  The streaming kernel unpacks the cache again for every 16 rows (two column tiles), the other one once for up to
-// 256, at a higher price per tile.  8 sequences of 12000 entries, 8 KV heads of 128, streaming / other: 24 rows 85 / 106 us,
-// 36 rows 117 / 107; 4 heads of 64: 24 rows 36 / 46, 36 rows 43 / 46, 52 rows 51 / 47.
-bool by_chunks(const Kv4& c, long long rows) { return rows > 32 && c.d != 256; }
+// 256, at a higher price per tile, and higher again where P has two terms.  8 sequences of 12000 entries, 8 KV heads of 128,
+// streaming / other: 24 rows 85 / 106 us, 36 rows 117 / 107 (float32 outputs 149 / 143), 52 rows 143 / 108 (187 / 145); 4 KV
+// heads, 35 rows, the drafts of the benchmark: 72 / 82 with float32 outputs.
+bool by_chunks(const Kv4& c, long long rows, bool two_terms) { return rows > (two_terms ? 48 : 32) && c.d != 256; }
 
 }  // namespace
 
@@ -536,7 +573,10 @@ int kv4_sm_count() {
 
 size_t kv4_attention_workspace(const Kv4& c, int max_q, int n_q_heads) {
   const long long rows = rows_of(c, true, max_q, n_q_heads);
-  return by_chunks(c, rows) ? kv4_chunk_workspace(c, nullptr, nullptr) : workspace(c, rows, rows <= 8 ? 1 : 2, nullptr, nullptr);
+  const size_t stream = workspace(c, rows, rows <= 8 ? 1 : 2, nullptr, nullptr);
+  if (!by_chunks(c, rows, false)) return stream;
+  const size_t chunk = kv4_chunk_workspace(c, nullptr, nullptr);
+  return by_chunks(c, rows, true) || chunk > stream ? chunk : stream;
 }
 
 extern "C" int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int dtype, const void* q, long long q_stride, int n_tokens,
@@ -565,7 +605,7 @@ extern "C" int im_kv4_attention(const im_kv4* cache, const im_kv4_map* map, int 
                 softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)c.d), {}};
   const long long rows = rows_of(c, cu_q != nullptr, max_q, n_q_heads);
   cudaStream_t s = (cudaStream_t)cuda_stream;
-  if (by_chunks(c, rows)) {
+  if (by_chunks(c, rows, out_f32 || dtype == IM_F16)) {
     kv4_chunk_workspace(c, (uint8_t*)workspace_, &a.ws);
     const cudaError_t e = kv4_launch_chunk(a, dtype, out_f32, q, out, lse, grid, s);
     return e == cudaSuccess ? IM_OK : im_fail_message(IM_ERR_CUDA, cudaGetErrorString(e));

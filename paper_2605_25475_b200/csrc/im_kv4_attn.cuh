@@ -14,6 +14,11 @@ struct Deal {
   long long q, rest;  // the first `rest` workers get q + 1 tiles, the others q
   int workers;
 };
+// Tensor cores cut off what does not fit their float32 accumulators: 1e-8 of the sum per step, always towards zero.  Where
+// outputs are float32 the accumulators are therefore emptied into the workspace (the place of the segment's partial result,
+// float32 additions) every FLUSH_STEPS steps; for 16-bit outputs the loss is far below their own rounding.
+constexpr int FLUSH_STEPS = 128;
+
 struct Piece {  // of a worker whose run begins inside an item: that item
   long long base;  // its first tile in the line; -1: the run begins with an item
   int tiles, rows;

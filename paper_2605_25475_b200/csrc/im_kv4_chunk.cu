@@ -28,6 +28,8 @@ constexpr int UNPACK_WARPS = 4, UNPACK = UNPACK_WARPS * 32;
 constexpr int W_COPY = 8, W_UNPACK = 9, W_MMA = W_UNPACK + UNPACK_WARPS, THREADS = (W_MMA + QT) * 32;
 constexpr int STAGES = 3, RAW = 5;
 constexpr int HALF_BYTES = KT * 128;  // 64 rows x 128 bytes (64 channels)
+template <bool TWO, typename OutT>  // tiles between two emptyings of the accumulators
+constexpr int flush_tiles() { return std::is_same<OutT, float>::value ? FLUSH_STEPS / (KT / 16 * (TWO ? 2 : 1)) : 1 << 30; }
 constexpr int S_COL = 0, P_COL = 128, O_COL = 256, TMEM_COLS = 512;
 
 template <int D>
@@ -129,6 +131,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* y) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]), "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]), "=r"(y[8]), "=r"(y[9]),
+        "=r"(y[10]), "=r"(y[11]), "=r"(y[12]), "=r"(y[13]), "=r"(y[14]), "=r"(y[15])
+      : "r"(taddr)
+      : "memory");
+}
 // One segment of a worker's run: tiles [tile, end) of an item.  Every role walks the run by itself.
 struct Walk {
   Seq s;
@@ -362,7 +373,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
 #pragma unroll
             for (int ks = 0; ks < KT / 16; ++ks)
               mma_ts(tmem + (uint32_t)(O_COL + x * 128), tmem + (uint32_t)(P_COL + 64 * x + 32 * (TWO ? term : cnt & 1) + 8 * ks),
-                     desc_sw128(va + ks * 2048, HALF_BYTES, 1024), idesc_o, (j | term | ks) ? 1u : 0u);
+                     desc_sw128(va + ks * 2048, HALF_BYTES, 1024), idesc_o, (j % flush_tiles<TWO, OutT>() | term | ks) ? 1u : 0u);
           mma_commit(smem_u32(&sh.pvdone[x]));
           if (j + 1 == nt) mma_commit(smem_u32(&sh.odone[x]));
           mma_commit(smem_u32(&sh.empty[n % STAGES]));
@@ -426,7 +437,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
         }
         const float f = row_factor(a, g.h, ex);
         const int lim_min = __reduce_min_sync(0xffffffffu, there ? lim : g.L);
-        float mref = NO_MAX;
+        constexpr int FLUSH = flush_tiles<TWO, OutT>();
+        float* pp = a.ws.part + ((size_t)(2 * worker + (t0 <= g.base ? 1 : 0)) * BLOCK_ROWS + x * ROWS + r) * (D + 4);
+        float mref = NO_MAX, fref = NO_MAX;  // fref: of what has been flushed to pp
         float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};  // the sum of p, in four parts
         for (int j = 0; j < nt; ++j) {
           const int k = cnt + j;
@@ -457,26 +470,44 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
           const float top = max3(m0, m1, fmaxf(m2, m3)) * f;
           const bool raise = top - mref > 15.0f;
           bool pv_waited = false;
+          if (FLUSH < (1 << 30) && j > 0 && j % FLUSH == 0) {  // empty the accumulators, which the product of this tile then overwrites
+            if (!mbar_wait(smem_u32(&sh.pvdone[x]), (uint32_t)((k - 1) & 1), abort_flag)) { ok = false; break; }
+            pv_waited = true;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const float by = j > FLUSH ? ex2(fref - mref) : 0.f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < D; c0 += 16) {
+              uint32_t y[16];
+              tmem_ld16(t_o + (uint32_t)c0, y);
+              if (there) {
+#pragma unroll
+                for (int b = 0; b < 16; b += 4) {
+                  float4 p = make_float4(__uint_as_float(y[b]), __uint_as_float(y[b + 1]), __uint_as_float(y[b + 2]), __uint_as_float(y[b + 3]));
+                  if (j > FLUSH) {
+                    const float4 q = *reinterpret_cast<const float4*>(pp + c0 + b);
+                    p = make_float4(fmaf(q.x, by, p.x), fmaf(q.y, by, p.y), fmaf(q.z, by, p.z), fmaf(q.w, by, p.w));
+                  }
+                  *reinterpret_cast<float4*>(pp + c0 + b) = p;
+                }
+              }
+            }
+            fref = mref;
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          }
           if (__any_sync(0xffffffffu, raise)) {
             const float next = raise ? top - 7.0f : mref;
             const float corr = ex2(mref - next);
             mref = next;
 #pragma unroll
             for (int b = 0; b < 2; ++b) l2[b].x *= corr, l2[b].y *= corr;
-            if (j >= 1) {  // O holds the products up to tile j - 1 (that of j - 2 is complete): wait for the last one, then scale the row
+            if (j % FLUSH) {  // O holds the products up to tile j - 1 (that of j - 2 is complete): wait for the last one, then scale the row
               if (!mbar_wait(smem_u32(&sh.pvdone[x]), (uint32_t)((k - 1) & 1), abort_flag)) { ok = false; break; }
               pv_waited = true;
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
               for (int c0 = 0; c0 < D; c0 += 16) {
                 uint32_t y[16];
-                asm volatile(
-                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
-                    "tcgen05.wait::ld.sync.aligned;"
-                    : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]), "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]), "=r"(y[8]), "=r"(y[9]),
-                      "=r"(y[10]), "=r"(y[11]), "=r"(y[12]), "=r"(y[13]), "=r"(y[14]), "=r"(y[15])
-                    : "r"(t_o + (uint32_t)c0)
-                    : "memory");
+                tmem_ld16(t_o + (uint32_t)c0, y);
 #pragma unroll
                 for (int b = 0; b < 16; ++b) y[b] = __float_as_uint(__uint_as_float(y[b]) * corr);
                 tmem_st16(t_o + (uint32_t)c0, y);
@@ -523,11 +554,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_chunk(const AttnArgs a, cons
         const size_t at = (size_t)(g.first + token) * a.H + head;
         const float inv = l == 0.f ? 0.f : kv4_pow2(kv4_exp(c.v_exp, g.h)) / l;
         OutT* op = out + at * D;
-        float* pp = a.ws.part + ((size_t)(2 * worker + (t0 <= g.base ? 1 : 0)) * BLOCK_ROWS + x * ROWS + r) * (D + 4);
+        const bool flushed = FLUSH < (1 << 30) && nt > FLUSH;
+        const float fby = flushed ? ex2(fref - mref) : 0.f;
 #pragma unroll
         for (int c0 = 0; c0 < D; c0 += 32) {
           float v[32];
           tmem_ld32(t_o + (uint32_t)c0, v);  // (warp-collective: rows that are not there load too, and store nothing)
+          if (flushed && there) {
+#pragma unroll
+            for (int b = 0; b < 32; ++b) v[b] = fmaf(pp[c0 + b], fby, v[b]);
+          }
           if (there && g.complete) {
 #pragma unroll
             for (int b = 0; b < 32; ++b) v[b] *= inv;
