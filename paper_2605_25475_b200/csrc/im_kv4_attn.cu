@@ -521,7 +521,7 @@ size_t workspace(const Kv4& c, long long rows, int nt, uint8_t* base, AttnWs* ws
   const int most = MOST_SMS * warps_of(c.d, nt);
   const size_t workers = tiles < most ? (size_t)tiles : (size_t)most;
   const size_t cum = 256, part = cum + kv4_align(8 * (size_t)c.n_seqs);
-  if (ws) *ws = {(Deal*)base, (long long*)(base + cum), nullptr, (float*)(base + part)};
+  if (ws) *ws = {(Deal*)base, (long long*)(base + cum), nullptr, (float*)(base + part), (int)workers};
   return part + kv4_align(2 * workers * 8 * nt * (c.d + 4) * 4);
 }
 

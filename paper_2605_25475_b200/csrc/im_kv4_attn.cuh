@@ -28,7 +28,8 @@ struct AttnWs {
   Deal* deal;
   long long* cum;  // [n_seqs] tiles ahead of the sequence (few rows: joined by query token), or
   Piece* piece;    // [workers] (many rows: joined by worker)
-  float* part;   // [2 * workers][ROWS][D + 4]
+  float* part;     // [2 * workers][ROWS][D + 4]
+  int workers;     // what the workspace has room for: the call may hold more tiles than its max_q says
 };
 struct AttnArgs {
   Kv4 c;
@@ -143,7 +144,7 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& a, int i) {
 }
 __device__ __forceinline__ long long work_of(const AttnArgs& a, const Seq& s) { return (long long)s.tiles * s.rb * a.c.Hkv; }
 
-// Adds the sequences up (every CTA for itself) and deals the line to at most `most` workers.  s_cum [THREADS + 1]: tiles
+// Adds the sequences up (every CTA for itself) and deals the line to at most `most` workers, and no more than the workspace holds.  s_cum [THREADS + 1]: tiles
 // ahead of each thread's run of `per` sequences.  Ends with a block barrier.
 template <int ROWS, int TILE, int THREADS>
 __device__ __forceinline__ Deal deal_line(const AttnArgs& a, long long* s_cum, long long* s_scan, long long most, int* workers, int* per_) {
@@ -165,7 +166,7 @@ __device__ __forceinline__ Deal deal_line(const AttnArgs& a, long long* s_cum, l
   if (tid == THREADS - 1) s_cum[THREADS] = before + incl;
   __syncthreads();
   const long long total = s_cum[THREADS];
-  *workers = (int)min(most, max(1ll, total));
+  *workers = (int)min(min(most, (long long)a.ws.workers), max(1ll, total));
   *per_ = per;
   Deal d;
   d.workers = *workers;

@@ -624,7 +624,7 @@ cudaError_t launch_types(const AttnArgs& a, int dtype, int out_f32, const void* 
 
 size_t kv4_chunk_workspace(const Kv4& c, uint8_t* base, AttnWs* ws) {
   const size_t piece = 256, part = piece + kv4_align(sizeof(Piece) * MOST_SMS);
-  if (ws) *ws = {(Deal*)base, nullptr, (Piece*)(base + piece), (float*)(base + part)};
+  if (ws) *ws = {(Deal*)base, nullptr, (Piece*)(base + piece), (float*)(base + part), MOST_SMS};
   return part + kv4_align(2 * (size_t)MOST_SMS * BLOCK_ROWS * (c.d + 4) * 4);
 }
 cudaError_t kv4_launch_chunk(const AttnArgs& a, int dtype, int out_f32, const void* q, void* out, float* lse, int grid, cudaStream_t s) {

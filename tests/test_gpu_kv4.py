@@ -378,6 +378,27 @@ def test_many_rows_agree_with_few_rows_over_a_long_cache(im, d, dtype):
     assert g.status() == 0
 
 
+@pytest.mark.parametrize("d,H,n,nq,L", [(64, 2, 1, 40, 70), (128, 4, 2, 24, 130), (256, 2, 1, 33, 100), (256, 8, 3, 200, 300)])
+@pytest.mark.parametrize("hint", [1, 2])
+def test_a_max_q_too_small_stays_inside_the_workspace(im, monkeypatch, d, H, n, nq, L, hint):
+    """The call holds more tiles than its max_q says and its workspace has partial results for: fewer workers share them.  The
+    bytes behind the workspace keep their pattern, and the results are right."""
+    pair = Pair(im, n, 6, 20, 2, d, 64, seed=6)
+    assert pair.append([L] * n)
+    ask, seen = pair.g._workspace, []
+
+    def guarded(*a):
+        _, nbytes = ask(*a)
+        seen.append((torch.full((nbytes + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda:0"), nbytes))
+        return seen[-1]
+
+    monkeypatch.setattr(pair.g, "_workspace", guarded)
+    for out_f32 in (False, True):
+        pair.attend([nq] * n, H, BF, out_f32, max_q=hint)
+    assert len(seen) == 2 and all(bool((ws[nbytes:] == 0xA5).all()) for ws, nbytes in seen)
+    assert pair.g.status() == 0
+
+
 @pytest.mark.parametrize("spread", [1e-30, 30.0, 1e4])
 def test_attention_of_extreme_queries(im, spread):
     """Queries far outside f16's range, and scores that pick one entry alone."""
