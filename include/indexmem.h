@@ -463,8 +463,10 @@ int im_state_import_head(im_ctx* ctx, int layer, int seq, int head, int which, c
  * All device pointers belong to the current device, all work is enqueued on `cuda_stream`; nothing synchronises, allocates
  * or depends on the host having seen a map, so every call can be captured into a CUDA graph and replayed.  A workspace
  * (256-byte aligned) holds what one call passes between its kernels: calls that may run at the same time, captured
- * ones included, need one each.  The sizes must fit: n_seqs <= 65535, n_kv_heads <= 256, n_pages * page_size and max_pages
- * * page_size below 2^31, max_pages * page_size * n_kv_heads * n_seqs below 2^36.
+ * ones included, need one each.  Calls that change maps which share refs must run one after the other (on one stream, or with
+ * events between streams): two at once would hand out the same pages.  The sizes must fit: n_seqs <= 65535, n_kv_heads <=
+ * 256, n_pages * page_size and max_pages * page_size at most 2^31 - 2^16, max_pages * page_size * n_kv_heads * n_seqs at most
+ * 2^36.
  */
 typedef enum im_dtype { IM_BF16 = 0, IM_F16 = 1, IM_F32 = 2 } im_dtype;
 

@@ -696,8 +696,9 @@ int kv4_describe(const im_kv4* p, const char* fn, Kv4* out) {
   if ((uintptr_t)p->pool & 15) return kv4_fail(IM_ERR_ARG, fn, "the pool must be 16-byte aligned");
   if (!im_kv4_page_bytes(p->n_kv_heads, p->head_dim, p->page_size))
     return kv4_fail(IM_ERR_ARG, fn, "head_dim must be 64, 128 or 256, page_size 16, 32, 64 or 128, n_kv_heads 1 to 256");
-  if (p->n_pages < 1 || (long long)p->n_pages * p->page_size > 0x7fffffffll || p->max_pages < 1 ||
-      (long long)p->max_pages * p->page_size > 0x7fffffffll || p->n_seqs < 1 || p->n_seqs > KV4_MAX_SEQS ||
+  // 2^16 below 31 bits: the kernels round lengths up to their tiles (up to 16384 entries) in 32 bits
+  if (p->n_pages < 1 || (long long)p->n_pages * p->page_size > 0x7fff0000ll || p->max_pages < 1 ||
+      (long long)p->max_pages * p->page_size > 0x7fff0000ll || p->n_seqs < 1 || p->n_seqs > KV4_MAX_SEQS ||
       (double)p->max_pages * p->page_size * p->n_kv_heads * p->n_seqs > 68719476736.0)
     return kv4_fail(IM_ERR_ARG, fn, "n_pages, max_pages or n_seqs out of range");
   *out = {(uint8_t*)p->pool, p->k_exp, p->v_exp, p->status, p->n_pages, p->page_size, p->n_kv_heads, p->head_dim, p->n_seqs, p->max_pages};

@@ -113,3 +113,14 @@ def test_gather_refusals(im):
     for kw in (dict(n=-1), dict(cu=None, n=5), dict(dt=3), dict(k=None, v=None), dict(k=FAKE + 8), dict(v=FAKE + 8)):
         assert g(**kw) == im.IM_ERR_ARG
     assert g(n=0, k=None, v=None) == im.IM_OK  # nothing to read
+
+
+@pytest.mark.parametrize("page_size", [16, 128])
+def test_lengths_leave_room_to_be_rounded_up(im, page_size):
+    """Kernels round a length up to their tiles in 32 bits: the last 2^16 lengths below 2^31 are refused."""
+    most = (2 ** 31 - 2 ** 16) // page_size
+    kw = dict(page_size=page_size, n_seqs=1, n_kv_heads=1)
+    for name in ("max_pages", "n_pages"):
+        for op in (0, 1, 2):
+            assert im._lib.im_kv4_workspace_bytes(ref(describe(im, **kw, **{name: most})), op, 1, 1) > 0
+            assert im._lib.im_kv4_workspace_bytes(ref(describe(im, **kw, **{name: most + 1})), op, 1, 1) == 0
