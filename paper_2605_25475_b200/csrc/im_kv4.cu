@@ -1,10 +1,9 @@
 // The paged 4-bit KV cache's calls other than attention: append (plan + store), gather, fork, compact (scan + plan +
 // move).  See include/indexmem.h for the contract and the format.
 //
-// All of them move bytes; the arithmetic of the quantiser hides behind its loads.  The integer part (which page goes
-// where) is one launch of eight CTAs that share their counts through distributed shared memory: the answer has to
-// be the same whatever order the hardware runs things in, so pages are ranked by prefix sums and nothing depends on the
-// order of atomics.
+// All of them move bytes.  The integer part (which page goes where) is one launch of one CTA, or of eight that share their
+// counts through distributed shared memory: the answer has to be the same whatever order the hardware runs things in, so
+// pages are ranked by prefix sums and nothing depends on the order of atomics.
 #include <cooperative_groups.h>
 #include <stdio.h>
 
@@ -71,7 +70,8 @@ __device__ __forceinline__ int new_tokens(const int32_t* cu, int i, int n_tokens
 
 // Gives out pages.  One cluster; the sequences' needs are added up by every CTA for itself (they are few), the free pages
 // are counted and listed by shares.  Phases are separated by cluster barriers, so that with from == to nothing is written
-// before everybody has read what the decision depends on.
+// before everybody has read what the decision depends on.  Bound by its chain of round trips (lengths, free pages, list,
+// rows): 9 to 12 us alone, for 32 sequences on 2,100 pages, 16 on 4,100.
 template <int MODE>
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_kv4_plan(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ cu, int n_tokens, PlanWs ws) {
@@ -357,7 +357,8 @@ k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict_
 
 // ------------------------------------------------------------------ gather
 // One thread per (row, head, 8 channels), keys and values: index in the order of the output, which is what most of the
-// bytes are, so that a warp writes 512 bytes side by side.
+// bytes are, so that a warp writes 512 bytes side by side.  131,072 rows of 8 heads of 128: 162 us to bf16 (4.2 TB/s, 64 % of
+// a copy), 251 us to float32 (4.9 TB/s, 74 %).
 constexpr int GATHER_THREADS = 256;
 template <typename T>
 __device__ __forceinline__ uint32_t pack_two(float a, float b);
@@ -430,7 +431,7 @@ k_kv4_gather(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict
 
 // ------------------------------------------------------------------ fork
 // refs of `to` start as those of `from`; then every row adds one to the pages of its new row and takes one off those of
-// its old row.  Integer sums: the order does not matter.
+// its old row.  Integer sums: the order does not matter.  Bound by its launches: 4.7 us for 1024 rows and refs apart.
 __global__ void k_kv4_copy_refs(const int32_t* __restrict__ a, int32_t* __restrict__ b, int n) {
   pdl_release();
   for (int p = blockIdx.x * blockDim.x + threadIdx.x; p < n; p += gridDim.x * blockDim.x) b[p] = a[p];
@@ -479,7 +480,7 @@ k_kv4_fork(Kv4 c, im_kv4_map from, im_kv4_map to, const int32_t* __restrict__ pa
 
 // ------------------------------------------------------------------ compact
 // Survivors of one sequence: their rows in the pool, in order, and the pages ahead of the first hole.  One block per
-// sequence, 16 flags per thread and round.
+// sequence, 16 flags per thread and round.  6 us for 2176 entries a sequence, 10 us for 32768: round trips.
 __global__ void __launch_bounds__(SCAN_THREADS)
 k_kv4_scan(Kv4 c, im_kv4_map from, const uint8_t* __restrict__ keep, int keep_stride, PlanWs ws) {
   __shared__ int s_warp[SCAN_THREADS / 32];
@@ -536,7 +537,9 @@ k_kv4_scan(Kv4 c, im_kv4_map from, const uint8_t* __restrict__ keep, int keep_st
 
 // A warp writes one group of 16 tokens of one head (18 d bytes side by side) from wherever its tokens were.  Every block has an equal
 // run of the groups to move, whatever the sequences are; the warps take the heads, and while a group moves the
-// places of the next one's tokens are fetched.
+// places of the next one's tokens are fetched.  One entry in four of 392,381 surviving, 8 heads of 128: 69 us, 302 MB of entries
+// (4.4 TB/s) and 387 MB of DRAM traffic (5.4 TB/s, 82 % of a copy), since a scale row of 8 bytes is read in sectors of 32.
+// Held to 40 registers, for half as many more warps, it spilled: the whole call took 102 us instead of 95.
 constexpr int MOVE_THREADS = 256;
 template <int D>
 __global__ void __launch_bounds__(MOVE_THREADS) k_kv4_move(Kv4 c, const int32_t* __restrict__ table, PlanWs ws) {

@@ -16,7 +16,11 @@
 //                by a power of two per row so that bf16 fits f16.
 // Tensor memory (512 columns): S_g at 64 g, P_g at 128 + 64 g (32 columns a term; one term: two buffers), O_g at 256 + 128 g.
 // With two buffers P needs no wait: S(j) is issued behind the product of tile j - 2, so who has seen S(j) may overwrite P(j - 2).
-// Every wait is bounded (IM_KV4_TIMEOUT).
+// Where outputs are float32 the accumulators are emptied every FLUSH_STEPS steps (im_kv4_attn.cuh).  Every wait is bounded
+// (IM_KV4_TIMEOUT).
+// 2048 queries x 16384 entries, 32 heads on 8 of 128: 554 us, 930 TF, 56 % of the measured bf16 rate.  A tile of 256 rows takes
+// 2100 cycles: 1024 of exponentials (16 per clock), 1280 of products, overlapped but for the chain barrier, load, maximum,
+// exponentials, store that every softmax thread runs through.  Tiles of 128 entries with P over S took 634 us.
 #include <math.h>
 
 #include "im_kv4_attn.cuh"
