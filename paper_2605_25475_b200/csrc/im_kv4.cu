@@ -272,7 +272,7 @@ __device__ __forceinline__ float2 two_floats<__half>(uint32_t v) {
 // writes the code rows of neighbouring tokens of one head, which lie side by side.  The rows of the grid behind those copy
 // the tokens of shared last pages.  The loads run ahead of the wait for the plan, and the lookups in its map (two round
 // trips) ahead of the quantiser.  Bound by the ALU pipe (70 % of it before finiteness went to one multiply-add per value, and the
-// maximum to three operands): 24,456 f16 tokens of 8 heads of 128, the append and its reading back, 81.5 -> 75.1 us.
+// maximum to three operands, 81.5 -> 75.1 us): 24,456 f16 tokens of 8 heads of 128, the append and its reading back, 70 us.
 constexpr int STORE_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(STORE_THREADS)
@@ -321,7 +321,8 @@ k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict_
   pdl_wait();
   if (i < 0) return;
   const int ok = *ws.ok, slot = lens[i] - (cu ? cu[i + 1] - t : 1);
-  const int page = ok && slot >= 0 && slot / c.ps < c.max_pages ? table[(size_t)i * c.max_pages + slot / c.ps] : -1;
+  const int nth = slot >= 0 ? kv4_nth_page(c, slot) : c.max_pages;
+  const int page = ok && nth < c.max_pages ? table[(size_t)i * c.max_pages + nth] : -1;
   bool odd = false;
   uint2 codes[2];
   uint8_t scale[2];
@@ -347,7 +348,7 @@ k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict_
   }
   if (odd) atomicOr(c.status, IM_KV4_NONFINITE);
   if (page < 0 || page >= c.n_pages) return;  // (the call is not made, as the plan has flagged)
-  const int at = slot % c.ps;
+  const int at = kv4_slot(c, slot);
   uint8_t* g = kv4_group(c, page, h, at >> 4);
   *reinterpret_cast<uint2*>(g + kv4_kc(c.d, at & 15) + 8 * blk) = codes[0];
   g[kv4_ks(c.d, at & 15) + blk] = scale[0];
@@ -357,8 +358,9 @@ k_kv4_store(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict_
 
 // ------------------------------------------------------------------ gather
 // One thread per (row, head, 8 channels), keys and values: index in the order of the output, which is what most of the
-// bytes are, so that a warp writes 512 bytes side by side.  131,072 rows of 8 heads of 128: 162 us to bf16 (4.2 TB/s, 64 % of
-// a copy), 251 us to float32 (4.9 TB/s, 74 %).
+// bytes are, so that a warp writes 512 bytes side by side.  Bound by issue slots (79 % busy
+// before the divisions by the page size became shifts).  131,072 rows of 8 heads of 128: 155 us to bf16 (4.4 TB/s, 68 % of a copy),
+// 265 us to float32 (4.6 TB/s, 70 %).
 constexpr int GATHER_THREADS = 256;
 template <typename T>
 __device__ __forceinline__ uint32_t pack_two(float a, float b);
@@ -411,10 +413,10 @@ k_kv4_gather(Kv4 c, const int32_t* __restrict__ table, const int32_t* __restrict
   if (!slots && cu) slot = r - cu[i];
   uint32_t kc = 0, vc = 0;
   uint8_t ks = 0, vs = 0;
-  if (slot >= 0 && slot < lens[i] && slot / c.ps < c.max_pages) {
-    const int page = table[(size_t)i * c.max_pages + slot / c.ps];
+  if (slot >= 0 && slot < lens[i] && kv4_nth_page(c, slot) < c.max_pages) {
+    const int page = table[(size_t)i * c.max_pages + kv4_nth_page(c, slot)];
     if (page >= 0 && page < c.n_pages) {
-      const int at = slot % c.ps;
+      const int at = kv4_slot(c, slot);
       const uint8_t* g = kv4_group(c, page, h, at >> 4);
       kc = *reinterpret_cast<const uint32_t*>(g + kv4_kc(c.d, at & 15) + 4 * x);
       ks = g[kv4_ks(c.d, at & 15) + (x >> 1)];
@@ -519,9 +521,9 @@ k_kv4_scan(Kv4 c, im_kv4_map from, const uint8_t* __restrict__ keep, int keep_st
     int chunk;
     int at = done + block_scan<SCAN_THREADS / 32>(__popc(flags), s_warp, &chunk);
     if (flags) {  // 16 entries starting at a multiple of 16 lie in one page
-      const int page = table[t0 / c.ps];
+      const int page = table[kv4_nth_page(c, t0)];
       if (page < 0 || page >= c.n_pages) bad = true;
-      const int r0 = page * c.ps + t0 % c.ps;
+      const int r0 = page * c.ps + kv4_slot(c, t0);
       for (uint32_t m = flags; m; m &= m - 1) ws.src[(size_t)i * ws.cap + at++] = r0 + __ffs(m) - 1;
     }
     done += chunk;
@@ -567,8 +569,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) k_kv4_move(Kv4 c, const int32_t*
     Group g;
     const int j0 = ws.info[i] * c.ps + (t - ws.goff[i]) * 16;
     g.rows = min(16, ws.cnt[i] - j0);
-    g.slot = j0 % c.ps;
-    g.page = table[(size_t)i * c.max_pages + j0 / c.ps];
+    g.slot = kv4_slot(c, j0);
+    g.page = table[(size_t)i * c.max_pages + kv4_nth_page(c, j0)];
     g.src = (lane & 15) < g.rows ? ws.src[(size_t)i * ws.cap + j0 + (lane & 15)] : 0;
     return g;
   };
@@ -584,12 +586,12 @@ __global__ void __launch_bounds__(MOVE_THREADS) k_kv4_move(Kv4 c, const int32_t*
       for (int q = 0; q < CODES / 32; ++q) {
         const int e = q * 32 + lane, which = e / (16 * ROW16), r = e / ROW16 % 16, x = e % ROW16;
         const int s = __shfl_sync(0xffffffffu, from, r);
-        const uint8_t* a = kv4_group(c, s / c.ps, h, (s % c.ps) >> 4) + (which ? kv4_vc(D, s & 15) : kv4_kc(D, s & 15)) + 16 * x;
+        const uint8_t* a = kv4_group(c, kv4_nth_page(c, s), h, kv4_slot(c, s) >> 4) + (which ? kv4_vc(D, s & 15) : kv4_kc(D, s & 15)) + 16 * x;
         code[q] = r < now.rows ? *reinterpret_cast<const uint4*>(a) : make_uint4(0u, 0u, 0u, 0u);
       }
       // scales: lane = (which, row), D / 16 bytes each
       const int which = lane >> 4, r = lane & 15;
-      const uint8_t* a = kv4_group(c, from / c.ps, h, (from % c.ps) >> 4) + (which ? kv4_vs(D, from & 15) : kv4_ks(D, from & 15));
+      const uint8_t* a = kv4_group(c, kv4_nth_page(c, from), h, kv4_slot(c, from) >> 4) + (which ? kv4_vs(D, from & 15) : kv4_ks(D, from & 15));
       uint32_t scale[D / 64];
 #pragma unroll
       for (int q = 0; q < D / 64; ++q) scale[q] = r < now.rows ? reinterpret_cast<const uint32_t*>(a)[q] : 0u;

@@ -24,6 +24,9 @@ __device__ __forceinline__ size_t kv4_group_index(const Kv4& c, int page, int h,
 __device__ __forceinline__ uint8_t* kv4_group(const Kv4& c, int page, int h, int group) {
   return c.pool + kv4_group_index(c, page, h, group) * kv4_group_bytes(c.d);
 }
+// entry t >= 0 of a sequence: which of its pages, and where in it (page sizes are powers of two; a division is 20 instructions)
+__device__ __forceinline__ int kv4_nth_page(const Kv4& c, int t) { return (int)((unsigned)t >> (31 - __clz(c.ps))); }
+__device__ __forceinline__ int kv4_slot(const Kv4& c, int t) { return t & (c.ps - 1); }
 // offsets inside a group: row r of the key codes / key scales / value codes / value scales
 __device__ __forceinline__ int kv4_kc(int d, int r) { return r * (d >> 1); }
 __device__ __forceinline__ int kv4_ks(int d, int r) { return 8 * d + r * (d >> 4); }
