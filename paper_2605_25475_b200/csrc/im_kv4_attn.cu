@@ -557,7 +557,7 @@ long long rows_of(const Kv4& c, bool ragged, int max_q, int n_q_heads) { return 
 // Which kernel.  The streaming kernel unpacks the cache again for every 16 rows (two column tiles), the other one once for up to
 // 256, at a higher price per tile, and higher again where P has two terms.  8 sequences of 12000 entries, 8 KV heads of 128,
 // streaming / other: 24 rows 85 / 106 us, 36 rows 117 / 107 (float32 outputs 149 / 143), 52 rows 143 / 108 (187 / 145); 4 KV
-// heads, 35 rows, the drafts of the benchmark: 72 / 82 with float32 outputs.
+// heads, 35 rows, 5 tokens of 7 heads each, 100,484 entries: 72 / 82 with float32 outputs.
 bool by_chunks(const Kv4& c, long long rows, bool two_terms) { return rows > (two_terms ? 48 : 32) && c.d != 256; }
 
 }  // namespace
